@@ -370,6 +370,104 @@ int adasd_update_thresholds(const adasd_state *st /* host */, int k_max, const i
                             uint32_t *status /* or NULL */, void *stream);
 
 /*
+ * Losses over vocabulary rows: what a training step (of the draft, so that it follows the target; of the target, on tokens that
+ * were generated with this library) or a caller that reports log-probabilities takes of the same rows of logits.
+ *
+ * All calls below describe their rows by an adasd_rows: B sequences of T positions with one token each.
+ *   position (b,t) : p = softmax(logits[b,t,:]), x = tokens[b,t];
+ *   logprob[b,t]   = ln p(x);   entropy[b,t] = H(p) in nats (Appendix A of the paper);
+ *   a position with weight[b,t] == 0 (or active[b,t] == 0) does not count: its logits, token and other inputs are not read (they
+ *   need not be numbers), its results are 0, and its row of dlogits is written with zeros;
+ *   status[b,t]    = ADASD_ST_BAD_TOKEN (token outside [0,V): log-probability NaN), ADASD_ST_NONFINITE (NaN/+inf in the row, or no
+ *                    logit above -2^120: results NaN), or 0.  A gradient row that depends on a NaN is NaN.
+ * Logits of -inf, or of the type's lowest value beside ordinary ones, are tokens without mass: gradient 0 there.
+ * Gradients have the type of the logits (formed in 32 bits, rounded once).  dlogits may be the logits' own memory (same pointer and
+ * strides: the gradient takes their place); any other overlap with logits the call reads is refused.
+ * Strides as everywhere here are in elements; rows may lie in either order (a [T,B,V] array seen as [B,T,V] is fine, and so is a
+ * view that leaves out positions) but must not overlap.  B*T <= ADASD_MAX_ROWS.  No call synchronises, allocates or keeps anything
+ * from one call for the next; sums are taken in a fixed order, so results are reproducible bit for bit.
+ */
+#define ADASD_MAX_ROWS (1 << 20)       /* positions of one log-probability or loss call */
+typedef struct {
+  /* inputs */
+  const void *logits;              /* [B, T, V] */
+  adasd_dtype dt;
+  int32_t B, T, V;
+  int64_t seq_stride, pos_stride;  /* elements between sequences / positions */
+  const int32_t *tokens;           /* [B, T] */
+  const float *weight;             /* [B, T] or NULL (1 everywhere): a loss is the sum of weight * term; losses only */
+  const uint8_t *active;           /* [B, T] or NULL (all); log-probability calls only */
+  /* outputs */
+  float *logprob;                  /* [B, T] or NULL */
+  float *entropy;                  /* [B, T] or NULL */
+  uint32_t *status;                /* [B, T] or NULL */
+  void *dlogits;                   /* [B, T, V], type of the logits, or NULL (no gradient wanted) */
+  int64_t d_seq_stride, d_pos_stride;
+  void *workspace;                 /* adasd_loss_workspace_bytes, 256-byte aligned, zeroed once by adasd_workspace_init */
+  size_t ws_bytes;
+} adasd_rows;
+
+/* Scratch of the calls below for B x T positions over V (serves any smaller B*T, and any V up to this one).  Calls that share
+ * one must be ordered on one stream. */
+int adasd_loss_workspace_bytes(int B, int T, int V, adasd_dtype dt, size_t *bytes /* host */);
+
+/* logprob, entropy and status of every active position (dlogits is not touched).  One read of the logits. */
+int adasd_token_logprob(const adasd_rows *rows /* host */, void *stream);
+
+/* The backward pass of the same: given dlogprob [B,T] and dentropy [B,T] (or NULL: 0), the derivatives of a loss by the two,
+ *   dlogits[b,t,j] = dlogprob (1[j = x] - p_j) - dentropy p_j (ln p_j + H).
+ * logprob, entropy and status are written too where given. */
+int adasd_token_logprob_grad(const adasd_rows *rows /* host */, const float *dlogprob, const float *dentropy /* or NULL */,
+                             void *stream);
+
+/*
+ * Clipped policy loss.  With r = exp(logprob - old_logprob) and the advantage A of the position,
+ *   term = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A) + kl_coef KL - entropy_coef H,   loss = sum over (b,t) of weight term,
+ *   KL   = exp(d) - 1 - d with d = ref_logprob - logprob (the sampled token's estimate), or, with ref_logits,
+ *          sum_j p_j (ln p_j - ln q_j) over the vocabulary (+inf where q_j = 0 < p_j; such a row's gradient is NaN), or 0 without
+ *          either.  (Both given: ADASD_ERR_INVALID_ARG.)
+ * Where A is 0 the first part is 0 whatever r is; a coefficient of 0 leaves its part out.  dlogits is the derivative of
+ * grad_scale * loss; at a border of the clipping the unclipped branch counts.
+ */
+typedef struct {
+  const float *advantage;          /* [B, T], or [B] with adv_per_seq */
+  int32_t adv_per_seq;
+  const float *old_logprob;        /* [B, T] or NULL: the tokens were drawn from these very rows (r = 1, gradient -A dlogprob) */
+  const float *ref_logprob;        /* [B, T] or NULL */
+  const void *ref_logits;          /* [B, T, V], type of the logits, or NULL */
+  int64_t r_seq_stride, r_pos_stride;
+  const float *grad_scale;         /* [1] or NULL (1) */
+  float clip_low, clip_high;       /* 0 <= clip_low <= 1, 0 <= clip_high (INFINITY: no upper border) */
+  float kl_coef, entropy_coef;     /* finite */
+  float *loss;                     /* [1] */
+  float *token_loss;               /* [B, T] or NULL: term */
+  float *kl;                       /* [B, T] or NULL */
+} adasd_policy_args;
+int adasd_policy_loss(const adasd_rows *rows /* host */, const adasd_policy_args *args /* host */, void *stream);
+
+/*
+ * Preference loss over P = B/2 pairs of sequences (B even): sequence i was preferred to sequence P + i.  With
+ *   score_b = sum_t weight (logprob - ref_logprob),   D = score_i - score_(P+i),
+ *   kind 0 (logistic): m = beta D - margin,  l = (1 - e) ln(1 + exp(-m)) + e ln(1 + exp(m)),  e = label_smoothing;
+ *   kind 1 (squared) : m = D - margin,       l = (m - 1/(2 beta))^2;
+ *   kind 2 (hinge)   : m = beta D - margin,  l = max(0, 1 - m)   (slope 0 at m = 1);
+ * loss = sum over the pairs of pair_weight l.  (weight = mask / length gives length-averaged scores; no ref_logprob a loss without
+ * a reference.)  dlogits is the derivative of grad_scale * loss; a pair with pair_weight 0 adds nothing and has zero gradient rows.
+ */
+typedef struct {
+  int32_t kind;
+  float beta, margin, label_smoothing;   /* beta > 0, finite; 0 <= label_smoothing <= 1 (kind 0 only) */
+  const float *ref_logprob;        /* [B, T] or NULL (0) */
+  const float *pair_weight;        /* [P] or NULL (1/P) */
+  const float *grad_scale;         /* [1] or NULL (1) */
+  float *loss;                     /* [1] */
+  float *pair_loss;                /* [P] or NULL: l */
+  float *pair_margin;              /* [P] or NULL: m */
+  float *score;                    /* [B] or NULL */
+} adasd_preference_args;
+int adasd_preference_loss(const adasd_rows *rows /* host */, const adasd_preference_args *args /* host */, void *stream);
+
+/*
  * Optional kernel timing for benchmarks (host side only; not for production loops).
  * adasd_profile_enable(n) creates n pairs of HIP events per kernel class and makes the entry points
  * hand one pair to each kernel launch (the dispatch stamps them at its start and end, so the
@@ -379,7 +477,7 @@ int adasd_update_thresholds(const adasd_state *st /* host */, int k_max, const i
  * the single-read path the one kernel of the whole statistics stage, class 1 then stays empty),
  * 1 JS distance (two-kernel path), 2 decision, 3 token sampling (a small round's decisions are taken in
  * the same kernel, class 2 then stays empty), 4 state update, 5 drafting calls
- * (adasd_draft_entropy and adasd_draft_step: one kernel per call), 6 adasd_stream_read.
+ * (adasd_draft_entropy and adasd_draft_step: one kernel per call), 6 adasd_stream_read, 7 log-probabilities and losses.
  * NOT thread-safe: there is one set of events per process, and while it is enabled every entry point
  * records into it.  Enable, the calls to be timed, read and disable must all come from one thread, with
  * no other thread inside the library meanwhile.  With timing disabled (the initial state) the entry

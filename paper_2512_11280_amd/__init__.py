@@ -9,4 +9,6 @@ from .binding import (AdasdError, Options, State, VerifyResult, draft_entropy, d
                       load_library, profile_disable, profile_enable, profile_read, stream_read,
                       update_thresholds, verify, workspace_bytes, Workspace, Shard, verify_shard_stats,
                       verify_shard_jsd, verify_shard_decide, verify_shard_sample, verify_shard_pick,
-                      verify_shard_refine, verify_shard_settle)
+                      verify_shard_refine, verify_shard_settle, LossWorkspace,
+                      token_logprob, token_logprob_grad, policy_loss, PolicyOptions, PolicyResult, preference_loss,
+                      PreferenceOptions, PreferenceResult)

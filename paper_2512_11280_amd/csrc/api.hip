@@ -13,24 +13,21 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 // ---- optional kernel timing ----------------------------------------------------------------
-constexpr int kClasses = 7;
+constexpr int kClasses = 8;
 struct Profiler {
   std::mutex mu;
   bool on = false;
   int cap = 0;
   std::vector<hipEvent_t> start[kClasses], stop[kClasses];
-  int used[kClasses] = {0, 0, 0, 0, 0, 0, 0};
+  int used[kClasses] = {};
 } g_prof;
 
 thread_local int t_class = -1;   // kernel class of the timing scope that is open on this thread
 
-struct Scope {   // the kernels launched while it lives are timed under class c
-  int prev;
-  Scope(int c, hipStream_t) : prev(t_class) { t_class = c; }
-  ~Scope() { t_class = prev; }
-};
-
 }  // namespace
+
+Scope::Scope(int c, hipStream_t) : prev(t_class) { t_class = c; }
+Scope::~Scope() { t_class = prev; }
 
 bool profile_take_events(hipEvent_t* start, hipEvent_t* stop) {
   if (!g_prof.on || t_class < 0) return false;

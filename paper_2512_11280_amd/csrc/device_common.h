@@ -58,6 +58,20 @@ __device__ __forceinline__ double log2_acc(float x) {
   return (double)e + (double)lg2(m);
 }
 
+// log2 of a positive finite float to about 1e-10: exponent, and the mantissa in [sqrt 1/2, sqrt 2) by the series of the area tangent,
+// ln((1 + f) / (1 - f)) = 2 (f + f^3/3 + f^5/5 + ...), |f| <= 0.172 (next term 4e-11).  Where results of many rows are added up.
+__device__ __forceinline__ double log2_fine(float x) {
+  int e;
+  double m = (double)__builtin_frexpf(x, &e);
+  if (m < 0.70710678118654752) {
+    m *= 2.0;
+    e -= 1;
+  }
+  const double f = (m - 1.0) / (m + 1.0), g = f * f;
+  const double p = fma(g, fma(g, fma(g, fma(g, fma(g, 1.0 / 11, 1.0 / 9), 1.0 / 7), 1.0 / 5), 1.0 / 3), 1.0);
+  return (double)e + (2.0 / 0.693147180559945309417232) * f * p;
+}
+
 // ---------------------------------------------------------------------------------------------
 // Issue order on gfx950, measured with one-instruction loops at eight wavefronts per SIMD.  A SIMD takes two
 // vector instructions at a time if they come from different wavefronts and at least one of them is plain

@@ -103,6 +103,11 @@ struct VerifyOut {
 // the launch carries a pair of events that the dispatch itself stamps at its start and end (the same
 // timestamps a profiler reports), so the measured durations hold no launch or queueing time.
 bool profile_take_events(hipEvent_t* start, hipEvent_t* stop);
+struct Scope {   // the kernels launched on this thread while it lives are timed under class c
+  int prev;
+  Scope(int c, hipStream_t);
+  ~Scope();
+};
 template <class Kernel, class... Args>
 inline void launch_kernel(Kernel kernel, dim3 grid, dim3 block, hipStream_t st, Args... args) {
   hipEvent_t e0, e1;
@@ -166,6 +171,60 @@ inline bool scan_prunes(int chunk, int dt) { return chunk * (dt == ADASD_BF16 ? 
 // Ragged windows: the positions i < draft_len[b] of all sequences, packed into slots[0 .. n) in the order
 // (window position, sequence), -1 in the remaining slots up to B*K (one small kernel).
 hipError_t launch_pack_slots(const int32_t* draft_len, int B, int K, int32_t* slots, hipStream_t st);
+
+// ---- log-probabilities and losses over vocabulary rows (loss.hip)
+struct RowPlace {       // where the rows [B, T, V] of an array lie
+  char* base;
+  int64_t seq, pos;     // elements
+};
+struct LossRows {
+  RowPlace z, ref, g;   // logits, the reference's (base null: none), gradient (base null: none)
+  const int32_t* tokens;
+  const float* weight;  // [n] or null
+  const uint8_t* active;
+  float* logprob;       // outputs [n], each may be null
+  float* entropy;
+  uint32_t* status;
+  int32_t T, V, n;      // n = B * T positions
+};
+enum LossKind : int32_t { kLogprob, kPolicy, kPreference };
+struct LossTerm {       // what the numbers of a position are formed from
+  LossKind kind;
+  // log-probabilities: derivatives of the caller's loss, or null (forward only)
+  const float* dlogprob;
+  const float* dentropy;
+  // policy
+  const float* advantage;
+  const float* old_logprob;
+  const float* ref_logprob;     // (preference too)
+  const float* grad_scale;      // (preference too)
+  int32_t adv_per_seq;
+  float clip_low, clip_high, kl_coef, entropy_coef;
+  float* token_loss;
+  float* kl;
+  float* loss;                  // (preference too)
+  // preference
+  int32_t pair_kind, P;
+  float beta, margin, smoothing;
+  const float* pair_weight;
+  float* pair_loss;
+  float* pair_margin;
+  float* score;
+};
+struct LossCoef {       // of a position: its gradient row is a 1[j = x] + 2^(x_j - m) (k0 + k1 (x_j - m) + k2 dd_j) (loss_device.h)
+  float m, a, k0, k1, k2, c, pad[2];
+};
+struct LossWorkspace {
+  LossCoef* coef;       // [n]
+  double* term;         // [n] what a position adds to the loss or to its sequence's score
+  double* pair;         // [n] what a pair adds to the loss
+  float* seq;           // [n] derivative of the loss by a sequence's score
+  float4* rec;          // [slices of all rows][2] sums of the slices
+};
+constexpr int kMaxLossRecords = 8 * 1792;      // slices beyond one per row (scan_split)
+size_t loss_workspace_bytes_for(size_t positions);
+size_t loss_workspace_layout(size_t ws_bytes, LossWorkspace* ws, void* base);
+hipError_t launch_loss(const LossRows& rows, int dt, const LossTerm& term, const LossWorkspace& ws, hipStream_t st);
 
 // plain streaming read (diagnostics): one word per workgroup goes to `sink`
 size_t stream_read_groups(size_t bytes);

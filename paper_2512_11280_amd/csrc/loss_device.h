@@ -1,0 +1,133 @@
+// Device helpers of the losses over vocabulary rows: partial sums of a slice of a row, their fold, and the gradient of a position.
+//
+// With x = z log2(e) (the float constant, see finish_loss_row) and m the largest x of the row, e_j = 2^(x_j - m):
+//   s = sum e_j,   u = sum (x_j - m) e_j            log-normaliser and entropy,
+//   w = sum e_j dd_j,  dd_j = (z_j - zr_j) log2(e) - c   (reference row zr, any constant c of the row) for the KL over the vocabulary.
+// The gradient of every loss here with respect to a row is
+//   dz_j = a 1[j = x] + e_j (k0 + k1 (x_j - m) + k2 dd_j)
+// with five numbers per position: a is the derivative by the token's log-probability, k0 gathers -a and the constants of the
+// entropy's and the KL's derivatives, k1 is the entropy's, k2 the KL's coefficient, all three over s.
+#pragma once
+#include "internal.h"
+#include "stats_device.h"
+
+namespace adasd {
+
+struct LossSums {          // of a slice
+  float m, s, u, w;        // of the row (w about the row's c)
+  float mr, sr;            // of the reference's row
+};
+__device__ __forceinline__ LossSums loss_empty() { return LossSums{kNegHuge, 0.f, 0.f, 0.f, kNegHuge, 0.f}; }
+
+// One vector of the row (and of the reference's) joins a lane's sums.  The vector's sums are formed on their own, so that a chain of
+// additions is one per vector long.
+template <int DT, bool REF>
+__device__ __forceinline__ void loss_push(LossSums& a, const uint4& x, const uint4& xr, float c) {
+  constexpr int EPV = Elem<DT>::per_vec;
+  const uint4 one[1] = {x};
+  const float m = fmaxf(a.m, vecs_max<DT, 1>(one)), d = a.m - m, f = ex2(d), neg_m = -m;
+  a.u = (a.u + d * a.s) * f;
+  a.s *= f;
+  if (REF) a.w *= f;
+  a.m = m;
+  float neg_mr = 0.f;
+  if (REF) {
+    const uint4 other[1] = {xr};
+    const float mr = fmaxf(a.mr, vecs_max<DT, 1>(other));
+    a.sr *= ex2(a.mr - mr);
+    a.mr = mr;
+    neg_mr = -mr;
+  }
+  float s[2] = {0.f, 0.f}, u[2] = {0.f, 0.f}, w[2] = {0.f, 0.f}, sr[2] = {0.f, 0.f};
+#pragma unroll
+  for (int g = 0; g < EPV / 4; ++g) {
+    float z[4], t[4], e[4];
+    unpack4<DT>(x, g, z);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = fma_log2e(z[i], neg_m);
+    ex2_group(t, e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[i & 1] += e[i];
+      u[i & 1] = fmaf(max_raw(t[i], -200.f), e[i], u[i & 1]);      // (masked logits: (-200) * 0 = 0; a NaN stays one through e)
+    }
+    if (REF) {
+      float y[4], tr[4], er[4];
+      unpack4<DT>(xr, g, y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tr[i] = fma_log2e(y[i], neg_mr);
+      ex2_group(tr, er);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sr[i & 1] += er[i];
+        const float dd = fma_log2e(z[i] - y[i], -c);
+        w[i & 1] = fmaf(e[i], e[i] > 0.f ? dd : 0.f, w[i & 1]);    // (without mass nothing is added, whatever the reference has there)
+      }
+    }
+  }
+  a.s += s[0] + s[1];
+  a.u += u[0] + u[1];
+  if (REF) {
+    a.w += w[0] + w[1];
+    a.sr += sr[0] + sr[1];
+  }
+}
+
+// One wavefront folds its lanes' sums; uniform results.
+template <bool REF> __device__ __forceinline__ LossSums loss_fold_wave(const LossSums& a) {
+  LossSums r = a;
+  r.m = wave_max_f(a.m);
+  const float d = r.m > kNegHuge ? a.m - r.m : 0.f, f = ex2(d);     // (nothing finite seen: the sums are 0, or a NaN)
+  r.s = wave_sum_f(a.s * f);
+  r.u = wave_sum_f((a.u + d * a.s) * f);
+  if (REF) {
+    r.w = wave_sum_f(a.w * f);
+    r.mr = wave_max_f(a.mr);
+    r.sr = wave_sum_f(a.sr * ex2(r.mr > kNegHuge ? a.mr - r.mr : 0.f));
+  }
+  return r;
+}
+
+// What the whole row's sums say, in nats and 64 bits.  The sums hold 2^(z k), k the float nearest log2(e): the row at a temperature
+// 1 / (1 + eps), eps = k ln 2 - 1 = -1.3e-8.  Dividing by k (and not by log2(e)) leaves an error of eps H in the
+// log-normaliser, which is put right; in the entropy it is of the size of eps.
+struct LossRow {
+  double lse, lse_ref;     // log-normalisers
+  double H, kl;
+  float inv_s;             // 1 / s
+  bool bad;
+};
+constexpr double kNat = 1.0 / (double)kLog2e;
+constexpr double kTemperature = (double)kLog2e * kLn2 - 1.0;
+template <bool REF> __device__ __forceinline__ LossRow finish_loss_row(const LossSums& t, float c) {
+  LossRow r;
+  const bool ok = t.s > 0.f && t.s < INFINITY && fabsf(t.u) < INFINITY && t.m > kNegHuge && t.m < INFINITY;
+  const double s = ok ? (double)t.s : (double)NAN, l2 = log2_fine((float)s);
+  r.H = fmax(kNat * (l2 - (double)t.u / s), 0.0);
+  r.H = ok ? r.H : (double)NAN;
+  r.lse = kNat * ((double)t.m + l2) + kTemperature * r.H;
+  r.inv_s = (float)(1.0 / s);
+  r.bad = !ok;
+  r.lse_ref = 0.0;
+  r.kl = 0.0;
+  if (REF) {
+    const bool okr = t.sr > 0.f && t.sr < INFINITY && t.mr > kNegHuge && t.mr < INFINITY;
+    const double l2r = log2_fine(okr ? t.sr : NAN);
+    r.lse_ref = kNat * ((double)t.mr + l2r);
+    // (c next to the normalisers' difference: both large where the rows carry different offsets)
+    r.kl = fmax(kNat * ((double)t.w / s + ((double)c - (((double)t.m - (double)t.mr) + (l2 - l2r)))), 0.0);
+    if (!ok || !okr || t.w != t.w) r.kl = (double)NAN;
+    r.bad = r.bad || !okr;
+  }
+  return r;
+}
+
+__device__ __forceinline__ bool position_counts(const LossRows& rows, int r) {
+  if (rows.weight) return rows.weight[r] != 0.f;
+  return rows.active ? rows.active[r] != 0 : true;
+}
+template <int DT> __device__ __forceinline__ const char* row_at(const RowPlace& p, int b, int t) {
+  return static_cast<const char*>(p.base) + ((int64_t)b * p.seq + (int64_t)t * p.pos) * Elem<DT>::bytes;
+}
+
+}  // namespace adasd
