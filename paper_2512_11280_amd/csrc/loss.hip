@@ -124,18 +124,23 @@ __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const 
   return k;
 }
 
+// The results of a position that does not count.
+__device__ __forceinline__ void report_nothing(const LossRows& rows, const LossTerm& f, const LossWorkspace& ws, int r) {
+  if (rows.logprob) rows.logprob[r] = 0.f;
+  if (rows.entropy) rows.entropy[r] = 0.f;
+  if (rows.status) rows.status[r] = 0u;
+  if (f.token_loss) f.token_loss[r] = 0.f;
+  if (f.kl) f.kl[r] = 0.f;
+  ws.term[r] = 0.0;
+}
+
 template <int DT, bool REF> __global__ void __launch_bounds__(kBlock) k_loss_rows(LossRows rows, LossTerm f, int S, LossWorkspace ws) {
   const int r = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (r >= rows.n) return;
   if (!position_counts(rows, r)) {
     if (lane == 0) {
-      if (rows.logprob) rows.logprob[r] = 0.f;
-      if (rows.entropy) rows.entropy[r] = 0.f;
-      if (rows.status) rows.status[r] = 0u;
-      if (f.token_loss) f.token_loss[r] = 0.f;
-      if (f.kl) f.kl[r] = 0.f;
+      report_nothing(rows, f, ws, r);
       ws.coef[r] = LossCoef{};
-      ws.term[r] = 0.0;
     }
     return;
   }
@@ -313,13 +318,94 @@ __global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int S, Loss
   }
 }
 
+// ---- Many rows: one workgroup per row, which stays in its registers (T threads, up to NB vectors each, raw) from the load to the
+// gradient: the logits are read once.
+template <int W> struct FusedLoss {
+  LossSums sums[W];
+  LossCoef coef;
+};
+template <int DT, bool ENT, int T, int NB>
+__global__ void __launch_bounds__(T) k_loss_fused(LossRows rows, LossTerm f, LossWorkspace ws) {
+  constexpr int EPV = Elem<DT>::per_vec, W = T / 64;
+  __shared__ FusedLoss<W> sh;
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = rows.V, whole = V / EPV, nv = vectors_of<DT>(V);
+  const int b = r / rows.T, t = r - b * rows.T;
+  char* out = const_cast<char*>(row_at<DT>(rows.g, b, t));
+  float g[EPV];
+  auto zeros = [&] {
+#pragma unroll
+    for (int i = 0; i < EPV; ++i) g[i] = 0.f;
+    for (int idx = tid; idx < nv; idx += T) store_grad<DT>(out, idx, V, g);
+  };
+  if (!position_counts(rows, r)) {
+    if (tid == 0) report_nothing(rows, f, ws, r);
+    zeros();
+    return;
+  }
+  const char* row = row_at<DT>(rows.z, b, t);
+  uint4 v[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const int idx = tid + j * T;
+    if ((j + 1) * T <= whole) v[j] = load_vec_any(row, idx);
+    else if (idx < nv) v[j] = load_vec_of<DT>(row, idx, V);
+    else v[j] = neutral_vec<DT>();
+  }
+  LossSums a = loss_empty();
+  a.m = vecs_max<DT, NB>(v);
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+    if (j * T < nv) loss_push_at<DT, false>(a, v[j], v[j], 0.f);
+  a = loss_fold_wave<false>(a);
+  if (lane == 0) sh.sums[wave] = a;
+  __syncthreads();
+  if (wave == 0) {
+    a = loss_fold_wave<false>(lane < W ? sh.sums[lane] : loss_empty());
+    if (lane == 0) {
+      double term;
+      sh.coef = settle_position<DT, false>(rows, f, r, a, 0.f, term);
+      if (f.loss) ws.term[r] = term;
+    }
+  }
+  __syncthreads();
+  const LossCoef k = sh.coef;
+  if (k.a == 0.f && k.k0 == 0.f && k.k1 == 0.f) {
+    zeros();
+    return;
+  }
+  const int x = rows.tokens[r];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const int idx = tid + j * T;
+    if (idx < nv) {
+      grad_vec<DT, ENT, false>(v[j], v[j], k, g);
+      if (idx == x / EPV) {
+#pragma unroll
+        for (int i = 0; i < EPV; ++i) g[i] += idx * EPV + i == x ? k.a : 0.f;
+      }
+      store_grad<DT>(out, idx, V, g);
+    }
+  }
+}
+
 }  // namespace
 
 hipError_t launch_loss(const LossRows& rows, int dt, const LossTerm& f, const LossWorkspace& ws, hipStream_t st) {
   const int n = rows.n, epv = dt == ADASD_BF16 ? 8 : 4, nv = (rows.V + epv - 1) / epv;
   const bool ref = rows.ref.base != nullptr;
   const dim3 block(kBlock);
-  if (n > 0) {
+  const bool ent = f.kind == kPolicy ? f.entropy_coef != 0.f : f.kind == kLogprob && f.dentropy;
+  const bool fused = rows.g.base && f.kind != kPreference && !ref && n >= 256 && nv <= 1024 * 20;
+  if (fused) {
+    const int NB = nv <= 1024 * 16 ? 16 : 20, T = NB == 20 ? 1024 : nv <= 128 * 16 ? 128 : nv <= 256 * 16 ? 256 : nv <= 512 * 16 ? 512 : 1024;
+#define ADASD_FUSED_CASE(DTV, ENTV, TV, NBV) \
+    if (dt == DTV && ent == ENTV && T == TV && NB == NBV) launch_kernel((k_loss_fused<DTV, ENTV, TV, NBV>), dim3(n), dim3(TV), st, rows, f, ws);
+#define ADASD_FUSED_CASES(TV, NBV) ADASD_FUSED_CASE(ADASD_BF16, false, TV, NBV) ADASD_FUSED_CASE(ADASD_BF16, true, TV, NBV) \
+    ADASD_FUSED_CASE(ADASD_F32, false, TV, NBV) ADASD_FUSED_CASE(ADASD_F32, true, TV, NBV)
+    ADASD_FUSED_CASES(128, 16) ADASD_FUSED_CASES(256, 16) ADASD_FUSED_CASES(512, 16) ADASD_FUSED_CASES(1024, 16) ADASD_FUSED_CASES(1024, 20)
+#undef ADASD_FUSED_CASES
+#undef ADASD_FUSED_CASE
+  } else if (n > 0) {
     const int S = scan_split(n, rows.V, dt);
     const dim3 grid(n, S), waves((n + kWaves - 1) / kWaves);
 #define ADASD_LOSS_CASE(DTV, REFV) \
@@ -333,7 +419,6 @@ hipError_t launch_loss(const LossRows& rows, int dt, const LossTerm& f, const Lo
     if (rows.g.base) {
       const int turns = 8, slices = (nv + turns * kBlock - 1) / (turns * kBlock);
       const dim3 pieces(n, slices);
-      const bool ent = f.kind == kPolicy ? f.entropy_coef != 0.f : f.kind == kLogprob && f.dentropy;
       const bool by_ref = ref && f.kl_coef != 0.f;
 #define ADASD_GRAD_CASE(DTV, ENTV, REFV) \
       if (dt == DTV && ent == ENTV && by_ref == REFV) \

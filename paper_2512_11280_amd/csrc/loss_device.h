@@ -19,25 +19,12 @@ struct LossSums {          // of a slice
 };
 __device__ __forceinline__ LossSums loss_empty() { return LossSums{kNegHuge, 0.f, 0.f, 0.f, kNegHuge, 0.f}; }
 
-// One vector of the row (and of the reference's) joins a lane's sums.  The vector's sums are formed on their own, so that a chain of
-// additions is one per vector long.
+// One vector of the row (and of the reference's) joins a lane's sums, about the references the sums have.  The vector's sums are
+// formed on their own, so that a chain of additions is one per vector long.
 template <int DT, bool REF>
-__device__ __forceinline__ void loss_push(LossSums& a, const uint4& x, const uint4& xr, float c) {
+__device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const uint4& xr, float c) {
   constexpr int EPV = Elem<DT>::per_vec;
-  const uint4 one[1] = {x};
-  const float m = fmaxf(a.m, vecs_max<DT, 1>(one)), d = a.m - m, f = ex2(d), neg_m = -m;
-  a.u = (a.u + d * a.s) * f;
-  a.s *= f;
-  if (REF) a.w *= f;
-  a.m = m;
-  float neg_mr = 0.f;
-  if (REF) {
-    const uint4 other[1] = {xr};
-    const float mr = fmaxf(a.mr, vecs_max<DT, 1>(other));
-    a.sr *= ex2(a.mr - mr);
-    a.mr = mr;
-    neg_mr = -mr;
-  }
+  const float neg_m = -a.m, neg_mr = -a.mr;
   float s[2] = {0.f, 0.f}, u[2] = {0.f, 0.f}, w[2] = {0.f, 0.f}, sr[2] = {0.f, 0.f};
 #pragma unroll
   for (int g = 0; g < EPV / 4; ++g) {
@@ -71,6 +58,24 @@ __device__ __forceinline__ void loss_push(LossSums& a, const uint4& x, const uin
     a.w += w[0] + w[1];
     a.sr += sr[0] + sr[1];
   }
+}
+
+// The same where the references follow the largest logits seen.
+template <int DT, bool REF>
+__device__ __forceinline__ void loss_push(LossSums& a, const uint4& x, const uint4& xr, float c) {
+  const uint4 one[1] = {x};
+  const float m = fmaxf(a.m, vecs_max<DT, 1>(one)), d = a.m - m, f = ex2(d);
+  a.u = (a.u + d * a.s) * f;
+  a.s *= f;
+  a.m = m;
+  if (REF) {
+    a.w *= f;
+    const uint4 other[1] = {xr};
+    const float mr = fmaxf(a.mr, vecs_max<DT, 1>(other));
+    a.sr *= ex2(a.mr - mr);
+    a.mr = mr;
+  }
+  loss_push_at<DT, REF>(a, x, xr, c);
 }
 
 // One wavefront folds its lanes' sums; uniform results.
