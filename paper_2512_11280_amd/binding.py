@@ -61,28 +61,6 @@ class _Shard(C.Structure):
     _fields_ = [("n_shards", C.c_int32), ("shard", C.c_int32), ("V_total", C.c_int32), ("col_begin", C.c_int32)]
 
 
-class _Rows(C.Structure):
-    _fields_ = [("logits", C.c_void_p), ("dt", C.c_int), ("B", C.c_int32), ("T", C.c_int32), ("V", C.c_int32),
-                ("seq_stride", C.c_int64), ("pos_stride", C.c_int64), ("tokens", C.c_void_p), ("weight", C.c_void_p),
-                ("active", C.c_void_p), ("logprob", C.c_void_p), ("entropy", C.c_void_p), ("status", C.c_void_p),
-                ("dlogits", C.c_void_p), ("d_seq_stride", C.c_int64), ("d_pos_stride", C.c_int64),
-                ("workspace", C.c_void_p), ("ws_bytes", C.c_size_t)]
-
-
-class _PolicyArgs(C.Structure):
-    _fields_ = [("advantage", C.c_void_p), ("adv_per_seq", C.c_int32), ("old_logprob", C.c_void_p),
-                ("ref_logprob", C.c_void_p), ("ref_logits", C.c_void_p), ("r_seq_stride", C.c_int64),
-                ("r_pos_stride", C.c_int64), ("grad_scale", C.c_void_p), ("clip_low", C.c_float), ("clip_high", C.c_float),
-                ("kl_coef", C.c_float), ("entropy_coef", C.c_float), ("loss", C.c_void_p), ("token_loss", C.c_void_p),
-                ("kl", C.c_void_p)]
-
-
-class _PreferenceArgs(C.Structure):
-    _fields_ = [("kind", C.c_int32), ("beta", C.c_float), ("margin", C.c_float), ("label_smoothing", C.c_float),
-                ("ref_logprob", C.c_void_p), ("pair_weight", C.c_void_p), ("grad_scale", C.c_void_p), ("loss", C.c_void_p),
-                ("pair_loss", C.c_void_p), ("pair_margin", C.c_void_p), ("score", C.c_void_p)]
-
-
 def library_path() -> str:
     return _LIB_PATH
 
@@ -125,10 +103,6 @@ def load_library():
                                           C.c_void_p, C.c_void_p, C.POINTER(_Options), C.c_void_p,
                                           C.c_void_p]
     L.adasd_loss_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
-    L.adasd_token_logprob.argtypes = [C.POINTER(_Rows), C.c_void_p]
-    L.adasd_token_logprob_grad.argtypes = [C.POINTER(_Rows), C.c_void_p, C.c_void_p, C.c_void_p]
-    L.adasd_policy_loss.argtypes = [C.POINTER(_Rows), C.POINTER(_PolicyArgs), C.c_void_p]
-    L.adasd_preference_loss.argtypes = [C.POINTER(_Rows), C.POINTER(_PreferenceArgs), C.c_void_p]
     L.adasd_stream_read.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p]
     L.adasd_profile_enable.argtypes = [C.c_int]
     L.adasd_profile_read.argtypes = [C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int)]
@@ -148,6 +122,9 @@ def _connect():
     native.connect(AdasdError, alloc_verify_result,
                    *(C.cast(getattr(L, "adasd_" + f), C.c_void_p).value
                      for f in ("draft_entropy", "draft_step", "verify", "verify_noalloc")))
+    native.connect_losses(PolicyResult, PreferenceResult,
+                          *(C.cast(getattr(L, "adasd_" + f), C.c_void_p).value
+                            for f in ("token_logprob", "token_logprob_grad", "policy_loss", "preference_loss")))
     _native = native
     return native
 
@@ -488,70 +465,12 @@ class LossWorkspace:
             _check(load_library().adasd_workspace_init(self.ptr, self.bytes, _stream()), "adasd_workspace_init")
 
 
-def _loss_rows(logits: torch.Tensor, tokens: torch.Tensor, workspace: LossWorkspace) -> tuple:
-    """(adasd_rows of the inputs, shape of the per-position outputs): logits [B, T, V] with tokens [B, T], or [B, V] with [B]."""
-    if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dim() not in (2, 3):
-        raise ValueError("logits must be a CUDA tensor [B, T, V] or [B, V]")
-    dt = _dtype_code(logits)
-    if logits.stride(-1) != 1 and logits.shape[-1] > 1:
-        raise ValueError("vocabulary dimension must be contiguous")
-    shape = tuple(logits.shape[:-1])
-    _need(tokens, torch.int32, "tokens")
-    if tuple(tokens.shape) != shape:
-        raise ValueError(f"tokens must be {list(shape)}, got {list(tokens.shape)}")
-    if tokens.device != logits.device or workspace.buf.device != logits.device:
-        raise ValueError(f"tokens and workspace must be on {logits.device}")
-    B, T = (shape[0], 1) if len(shape) == 1 else shape
-    V = logits.shape[-1]
-    a = _Rows(logits.data_ptr(), dt, B, T, V, logits.stride(0), logits.stride(1) if len(shape) == 2 else V, tokens.data_ptr())
-    a.workspace, a.ws_bytes = workspace.ptr, workspace.bytes
-    return a, shape
-
-
-def _shaped(t: Optional[torch.Tensor], dtype, shape, like: torch.Tensor, name: str):
-    """Data pointer of an optional contiguous input of this shape on the logits' device."""
-    if t is None:
-        return None
-    _need(t, dtype, name)
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
-    if t.device != like.device:
-        raise ValueError(f"{name} must be on {like.device}")
-    return t.data_ptr()
-
-
-def _out(t: Optional[torch.Tensor], dtype, shape, like: torch.Tensor, name: str) -> torch.Tensor:
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
-    _shaped(t, dtype, shape, like, name)
-    return t
-
-
-def _gradient(a: _Rows, dlogits: Optional[torch.Tensor], logits: torch.Tensor) -> torch.Tensor:
-    """The caller's gradient tensor, checked (any strides with a contiguous vocabulary), or a new one."""
-    if dlogits is None:
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    elif (not dlogits.is_cuda or dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.device != logits.device
-          or (dlogits.stride(-1) != 1 and dlogits.shape[-1] > 1)):
-        raise ValueError("dlogits must have the shape, type and device of the logits and a contiguous vocabulary")
-    a.dlogits, a.d_seq_stride = dlogits.data_ptr(), dlogits.stride(0)
-    a.d_pos_stride = dlogits.stride(1) if dlogits.dim() == 3 else a.V
-    return dlogits
-
-
 def token_logprob(logits: torch.Tensor, tokens: torch.Tensor, workspace: LossWorkspace, active: Optional[torch.Tensor] = None,
                   logprob_out: Optional[torch.Tensor] = None, entropy_out: Optional[torch.Tensor] = None,
                   status_out: Optional[torch.Tensor] = None):
     """adasd_token_logprob: ln softmax(logits)[token] and the entropy of every position of logits [B, T, V] (tokens [B, T]), or
     of single tokens, logits [B, V] (tokens [B]).  Returns (logprob, entropy, status)."""
-    a, shape = _loss_rows(logits, tokens, workspace)
-    a.active = _shaped(active, torch.uint8, shape, logits, "active")
-    logprob, entropy = (_out(t, torch.float32, shape, logits, n) for t, n in ((logprob_out, "logprob_out"), (entropy_out, "entropy_out")))
-    status = _out(status_out, torch.int32, shape, logits, "status_out")
-    a.logprob, a.entropy, a.status = logprob.data_ptr(), entropy.data_ptr(), status.data_ptr()
-    with torch.cuda.device(logits.device):
-        _check(load_library().adasd_token_logprob(C.byref(a), _stream()), "adasd_token_logprob")
-    return logprob, entropy, status
+    return (_native or _connect()).token_logprob(logits, tokens, workspace, active, logprob_out, entropy_out, status_out)
 
 
 def token_logprob_grad(logits: torch.Tensor, tokens: torch.Tensor, workspace: LossWorkspace, dlogprob: torch.Tensor,
@@ -559,14 +478,7 @@ def token_logprob_grad(logits: torch.Tensor, tokens: torch.Tensor, workspace: Lo
                        dlogits: Optional[torch.Tensor] = None) -> torch.Tensor:
     """adasd_token_logprob_grad: the gradient of a loss by the logits, given its derivatives by token_logprob's log-probabilities and
     entropies.  dlogits may be `logits` itself.  Pass it on with ``logits.backward(dlogits)``."""
-    a, shape = _loss_rows(logits, tokens, workspace)
-    a.active = _shaped(active, torch.uint8, shape, logits, "active")
-    dlp = _shaped(dlogprob, torch.float32, shape, logits, "dlogprob")
-    dent = _shaped(dentropy, torch.float32, shape, logits, "dentropy")
-    dlogits = _gradient(a, dlogits, logits)
-    with torch.cuda.device(logits.device):
-        _check(load_library().adasd_token_logprob_grad(C.byref(a), dlp, dent, _stream()), "adasd_token_logprob_grad")
-    return dlogits
+    return (_native or _connect()).token_logprob_grad(logits, tokens, workspace, dlogprob, dentropy, active, dlogits)
 
 
 @dataclass
@@ -597,38 +509,13 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, advantage: torch.Ten
     by the logits in the same call.  advantage: [B, T], or [B] for one per sequence; KL against ref_logprob [B, T] (the sampled
     tokens' estimate) or ref_logits [B, T, V] (over the vocabulary).  dlogits may be `logits` itself; grad_scale: one float on
     the device (a loss scale).  Pass the gradient on with ``logits.backward(result.dlogits)``."""
-    a, shape = _loss_rows(logits, tokens, workspace)
-    o = options or PolicyOptions()
-    a.weight = _shaped(weight, torch.float32, shape, logits, "weight")
-    per_seq = len(shape) == 2 and isinstance(advantage, torch.Tensor) and advantage.dim() == 1
-    p = _PolicyArgs(_shaped(advantage, torch.float32, shape[:1] if per_seq else shape, logits, "advantage"), int(per_seq),
-                    _shaped(old_logprob, torch.float32, shape, logits, "old_logprob"),
-                    _shaped(ref_logprob, torch.float32, shape, logits, "ref_logprob"))
-    if ref_logits is not None:
-        if (ref_logits.dtype != logits.dtype or ref_logits.shape != logits.shape or ref_logits.device != logits.device
-                or (ref_logits.stride(-1) != 1 and ref_logits.shape[-1] > 1)):
-            raise ValueError("ref_logits must have the shape, type and device of the logits and a contiguous vocabulary")
-        p.ref_logits, p.r_seq_stride = ref_logits.data_ptr(), ref_logits.stride(0)
-        p.r_pos_stride = ref_logits.stride(1) if ref_logits.dim() == 3 else a.V
-    p.grad_scale = _shaped(grad_scale, torch.float32, (1,), logits, "grad_scale")
-    p.clip_low, p.clip_high, p.kl_coef, p.entropy_coef = o.clip_low, o.clip_high, o.kl_coef, o.entropy_coef
-    f = dict(dtype=torch.float32, device=logits.device)
-    r = PolicyResult(torch.empty((), **f), torch.empty(shape, **f), torch.empty(shape, **f), torch.empty(shape, **f),
-                     torch.empty(shape, **f), torch.empty(shape, dtype=torch.int32, device=logits.device),
-                     _gradient(a, dlogits, logits) if need_grad else None)
-    a.logprob, a.entropy, a.status = r.logprob.data_ptr(), r.entropy.data_ptr(), r.status.data_ptr()
-    p.loss, p.token_loss, p.kl = r.loss.data_ptr(), r.token_loss.data_ptr(), r.kl.data_ptr()
-    with torch.cuda.device(logits.device):
-        _check(load_library().adasd_policy_loss(C.byref(a), C.byref(p), _stream()), "adasd_policy_loss")
-    return r
-
-
-PREFERENCE_KINDS = {"logistic": 0, "squared": 1, "hinge": 2}
+    return (_native or _connect()).policy_loss(logits, tokens, advantage, workspace, weight, old_logprob, ref_logprob, ref_logits,
+                                               options, grad_scale, need_grad, dlogits)
 
 
 @dataclass
 class PreferenceOptions:
-    kind: str = "logistic"
+    kind: str = "logistic"        # or "squared", "hinge"
     beta: float = 0.1
     margin: float = 0.0
     label_smoothing: float = 0.0
@@ -652,27 +539,8 @@ def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, workspace: LossW
     """adasd_preference_loss over P pairs: logits [2P, T, V] and tokens [2P, T], the P preferred sequences first.  weight [2P, T]: a mask
     (or mask / length for averaged scores); ref_logprob [2P, T]; pair_weight [P] (None: 1/P).  dlogits may be `logits` itself.  Pass
     the gradient on with ``logits.backward(result.dlogits)``."""
-    if not isinstance(logits, torch.Tensor) or logits.dim() != 3:
-        raise ValueError("logits must be a CUDA tensor [2P, T, V]")
-    a, shape = _loss_rows(logits, tokens, workspace)
-    o = options or PreferenceOptions()
-    if o.kind not in PREFERENCE_KINDS:
-        raise ValueError(f"kind must be one of {sorted(PREFERENCE_KINDS)}")
-    P = shape[0] // 2
-    a.weight = _shaped(weight, torch.float32, shape, logits, "weight")
-    p = _PreferenceArgs(PREFERENCE_KINDS[o.kind], o.beta, o.margin, o.label_smoothing,
-                        _shaped(ref_logprob, torch.float32, shape, logits, "ref_logprob"),
-                        _shaped(pair_weight, torch.float32, (P,), logits, "pair_weight"),
-                        _shaped(grad_scale, torch.float32, (1,), logits, "grad_scale"))
-    f = dict(dtype=torch.float32, device=logits.device)
-    r = PreferenceResult(torch.empty((), **f), torch.empty(P, **f), torch.empty(P, **f), torch.empty(shape[0], **f),
-                         torch.empty(shape, **f), torch.empty(shape, dtype=torch.int32, device=logits.device),
-                         _gradient(a, dlogits, logits) if need_grad else None)
-    a.logprob, a.status = r.logprob.data_ptr(), r.status.data_ptr()
-    p.loss, p.pair_loss, p.pair_margin, p.score = r.loss.data_ptr(), r.pair_loss.data_ptr(), r.margin.data_ptr(), r.score.data_ptr()
-    with torch.cuda.device(logits.device):
-        _check(load_library().adasd_preference_loss(C.byref(a), C.byref(p), _stream()), "adasd_preference_loss")
-    return r
+    return (_native or _connect()).preference_loss(logits, tokens, workspace, weight, ref_logprob, pair_weight, options, grad_scale,
+                                                   need_grad, dlogits)
 
 
 def stream_read(src: torch.Tensor, sink: torch.Tensor):

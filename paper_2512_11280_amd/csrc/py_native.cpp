@@ -10,6 +10,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -23,9 +24,14 @@ struct Abi {
   decltype(&adasd_draft_step) draft_step;
   decltype(&adasd_verify) verify;
   decltype(&adasd_verify_noalloc) verify_noalloc;
+  decltype(&adasd_token_logprob) token_logprob;
+  decltype(&adasd_token_logprob_grad) token_logprob_grad;
+  decltype(&adasd_policy_loss) policy_loss;
+  decltype(&adasd_preference_loss) preference_loss;
 } g_abi;
 PyObject* g_error = nullptr;         // AdasdError(code, where)
 PyObject* g_alloc_result = nullptr;  // alloc_verify_result(B, K, device)
+PyObject* g_policy_result = nullptr, *g_preference_result = nullptr;   // PolicyResult, PreferenceResult
 
 struct Fail {};                      // a Python exception is set
 
@@ -177,7 +183,9 @@ struct Names {
            *base_test = intern("base_test"), *reject_rule = intern("reject_rule"), *kde_min_n = intern("kde_min_n"),
            *bw_rule = intern("bw_rule"), *relaxed_off = intern("relaxed_off"), *d_eps = intern("d_eps"),
            *stats_path = intern("stats_path"), *apply_update = intern("apply_update"), *list_update = intern("list_update"),
-           *wait_polls = intern("wait_polls");
+           *wait_polls = intern("wait_polls"), *buf = intern("buf"), *clip_low = intern("clip_low"), *clip_high = intern("clip_high"),
+           *kl_coef = intern("kl_coef"), *entropy_coef = intern("entropy_coef"), *kind = intern("kind"), *beta = intern("beta"),
+           *margin = intern("margin"), *label_smoothing = intern("label_smoothing");
 };
 Names* N = nullptr;
 
@@ -369,6 +377,279 @@ PyObject* py_verify(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject
   });
 }
 
+// ---- log-probabilities and losses over vocabulary rows
+
+bool given(PyObject* o) { return o && o != Py_None; }
+float float_attr(PyObject* from, PyObject* name) {
+  const double v = PyFloat_AsDouble(Ref(from, name).o);
+  if (v == -1.0 && PyErr_Occurred()) throw Fail{};
+  return (float)v;
+}
+
+// The rows of a call: logits [B, T, V] with tokens [B, T], or [B, V] with [B]; outputs are allocated in the shape of the tokens.
+struct RowsCall {
+  adasd_rows rows{};
+  const at::Tensor* z;
+  int64_t shape[2];
+  int dims;
+  void* stream;
+  c10::hip::OptionalHIPGuard guard;       // the calls run on the logits' device, whatever the current one is
+
+  RowsCall(PyObject* logits, PyObject* tokens, PyObject* workspace, bool only_sequences) {
+    if (!THPVariable_Check(logits) || (z = &THPVariable_Unpack(logits), (z->dim() != 3 && (only_sequences || z->dim() != 2))) || !z->is_cuda())
+      fail(PyExc_ValueError, only_sequences ? "logits must be a CUDA tensor [2P, T, V]" : "logits must be a CUDA tensor [B, T, V] or [B, V]");
+    rows.dt = logits_type(logits);
+    dims = (int)z->dim() - 1;
+    const int64_t V = z->size(dims);
+    if (V > 1 && z->stride(dims) != 1) fail(PyExc_ValueError, "vocabulary dimension must be contiguous");
+    shape[0] = z->size(0);
+    shape[1] = dims == 2 ? z->size(1) : 1;
+    if (shape[0] > INT32_MAX || shape[1] > INT32_MAX || V > INT32_MAX) fail(PyExc_ValueError, "logits have too many positions");
+    rows.B = (int32_t)shape[0];
+    rows.T = (int32_t)shape[1];
+    rows.V = (int32_t)V;
+    rows.logits = z->data_ptr();
+    rows.seq_stride = z->stride(0);
+    rows.pos_stride = dims == 2 ? z->stride(1) : V;
+    rows.tokens = (const int32_t*)input(tokens, at::kInt, "tokens");
+    Ref buf(workspace, N->buf);
+    if (tensor(buf.o, "workspace.buf").device() != z->device()) fail(PyExc_ValueError, "workspace must be on the logits' device");
+    rows.workspace = (void*)int_attr(workspace, N->ptr);
+    rows.ws_bytes = int_attr(workspace, N->bytes);
+    guard.set_index(z->get_device());
+    stream = ::stream();
+  }
+  // A contiguous input of this shape on the logits' device.
+  void* input(PyObject* o, at::ScalarType type, const char* name, const int64_t* size, int n) const {
+    const at::Tensor& t = tensor(o, name);
+    if (!t.is_cuda() || t.scalar_type() != type || !t.is_contiguous()) {
+      PyErr_Format(PyExc_ValueError, "%s must be a contiguous CUDA tensor of %s", name, type_name(type));
+      throw Fail{};
+    }
+    bool same = t.dim() == n;
+    for (int i = 0; same && i < n; ++i) same = t.size(i) == size[i];
+    if (!same || t.device() != z->device()) {
+      PyErr_Format(PyExc_ValueError, n == 2 ? "%s must be [%lld, %lld] on the logits' device" : "%s must be [%lld] on the logits' device", name,
+                   (long long)size[0], n == 2 ? (long long)size[1] : 0ll);
+      throw Fail{};
+    }
+    return t.data_ptr();
+  }
+  void* input(PyObject* o, at::ScalarType type, const char* name) const { return input(o, type, name, shape, dims); }
+  void* maybe(PyObject* o, at::ScalarType type, const char* name) const { return given(o) ? input(o, type, name) : nullptr; }
+  const float* one(PyObject* o, int64_t n, const char* name) const { return given(o) ? (const float*)input(o, at::kFloat, name, &n, 1) : nullptr; }
+
+  // The gradient: the caller's tensor (any strides with a contiguous vocabulary), or a new one.  New reference.
+  PyObject* gradient(PyObject* o) {
+    if (given(o)) {
+      const at::Tensor& g = tensor(o, "dlogits");
+      if (g.device() != z->device() || g.scalar_type() != z->scalar_type() || g.sizes() != z->sizes() || (rows.V > 1 && g.stride(dims) != 1))
+        fail(PyExc_ValueError, "dlogits must have the shape, type and device of the logits and a contiguous vocabulary");
+      place(g);
+      Py_INCREF(o);
+      return o;
+    }
+    at::Tensor g = at::empty(z->sizes(), z->options());
+    place(g);
+    return wrap(std::move(g));
+  }
+  void place(const at::Tensor& g) {
+    rows.dlogits = g.data_ptr();
+    rows.d_seq_stride = g.stride(0);
+    rows.d_pos_stride = dims == 2 ? g.stride(1) : rows.V;
+  }
+  static PyObject* wrap(at::Tensor t) {
+    PyObject* o = THPVariable_Wrap(std::move(t));
+    if (!o) throw Fail{};
+    return o;
+  }
+};
+
+// Objects to be handed over together.
+template <int M> struct Objects {
+  PyObject* o[M] = {};
+  int n = 0;
+  ~Objects() {
+    for (int i = 0; i < n; ++i) Py_XDECREF(o[i]);
+  }
+  void add(PyObject* p) { o[n++] = p; }
+  template <class T> T* make(const RowsCall& c, at::IntArrayRef size, at::ScalarType type) {
+    at::Tensor t = at::empty(size, c.z->options().dtype(type));
+    T* p = (T*)t.data_ptr();
+    add(RowsCall::wrap(std::move(t)));
+    return p;
+  }
+  template <class T> T* take(const RowsCall& c, PyObject* o, at::ScalarType type, const char* name) {     // the caller's, or a new one
+    if (!given(o)) return make<T>(c, at::IntArrayRef(c.shape, c.dims), type);
+    T* p = (T*)c.input(o, type, name);
+    Py_INCREF(o);
+    add(o);
+    return p;
+  }
+  PyObject* tuple() {
+    PyObject* r = PyTuple_New(n);
+    if (!r) throw Fail{};
+    for (int i = 0; i < n; ++i) PyTuple_SET_ITEM(r, i, o[i]);
+    n = 0;
+    return r;
+  }
+  PyObject* call(PyObject* type) {
+    PyObject* r = PyObject_Vectorcall(type, o, n, nullptr);
+    if (!r) throw Fail{};
+    return r;
+  }
+};
+template <class F> void enqueue(const char* where, F f) {
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f();
+  Py_END_ALLOW_THREADS
+  check(rc, where);
+}
+bool truth(PyObject* o, bool fallback) {
+  if (!o) return fallback;
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Fail{};
+  return v != 0;
+}
+
+PyObject* py_token_logprob(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  return guarded([&]() -> PyObject* {
+    static PyObject* const names[] = {intern("logits"), intern("tokens"), intern("workspace"), intern("active"),
+                                      intern("logprob_out"), intern("entropy_out"), intern("status_out")};
+    PyObject* a[7];
+    parse("token_logprob", names, 3, args, nargs, kw, a);
+    RowsCall c(a[0], a[1], a[2], false);
+    c.rows.active = (const uint8_t*)c.maybe(a[3], at::kByte, "active");
+    Objects<3> out;
+    c.rows.logprob = out.take<float>(c, a[4], at::kFloat, "logprob_out");
+    c.rows.entropy = out.take<float>(c, a[5], at::kFloat, "entropy_out");
+    c.rows.status = out.take<uint32_t>(c, a[6], at::kInt, "status_out");
+    enqueue("adasd_token_logprob", [&] { return g_abi.token_logprob(&c.rows, c.stream); });
+    return out.tuple();
+  });
+}
+
+PyObject* py_token_logprob_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  return guarded([&]() -> PyObject* {
+    static PyObject* const names[] = {intern("logits"), intern("tokens"), intern("workspace"), intern("dlogprob"),
+                                      intern("dentropy"), intern("active"), intern("dlogits")};
+    PyObject* a[7];
+    parse("token_logprob_grad", names, 4, args, nargs, kw, a);
+    RowsCall c(a[0], a[1], a[2], false);
+    const float* dlp = (const float*)c.input(a[3], at::kFloat, "dlogprob");
+    const float* dent = (const float*)c.maybe(a[4], at::kFloat, "dentropy");
+    c.rows.active = (const uint8_t*)c.maybe(a[5], at::kByte, "active");
+    Objects<1> out;
+    out.add(c.gradient(a[6]));
+    enqueue("adasd_token_logprob_grad", [&] { return g_abi.token_logprob_grad(&c.rows, dlp, dent, c.stream); });
+    out.n = 0;
+    return out.o[0];
+  });
+}
+
+PyObject* py_policy_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  return guarded([&]() -> PyObject* {
+    static PyObject* const names[] = {intern("logits"), intern("tokens"), intern("advantage"), intern("workspace"), intern("weight"),
+                                      intern("old_logprob"), intern("ref_logprob"), intern("ref_logits"), intern("options"),
+                                      intern("grad_scale"), intern("need_grad"), intern("dlogits")};
+    PyObject* a[12];
+    parse("policy_loss", names, 4, args, nargs, kw, a);
+    RowsCall c(a[0], a[1], a[3], false);
+    adasd_policy_args p{};
+    p.adv_per_seq = c.dims == 2 && tensor(a[2], "advantage").dim() == 1;
+    p.advantage = p.adv_per_seq ? c.one(a[2], c.shape[0], "advantage") : (const float*)c.input(a[2], at::kFloat, "advantage");
+    c.rows.weight = (const float*)c.maybe(a[4], at::kFloat, "weight");
+    p.old_logprob = (const float*)c.maybe(a[5], at::kFloat, "old_logprob");
+    p.ref_logprob = (const float*)c.maybe(a[6], at::kFloat, "ref_logprob");
+    if (given(a[7])) {
+      const at::Tensor& q = tensor(a[7], "ref_logits");
+      if (q.device() != c.z->device() || q.scalar_type() != c.z->scalar_type() || q.sizes() != c.z->sizes() ||
+          (c.rows.V > 1 && q.stride(c.dims) != 1))
+        fail(PyExc_ValueError, "ref_logits must have the shape, type and device of the logits and a contiguous vocabulary");
+      p.ref_logits = q.data_ptr();
+      p.r_seq_stride = q.stride(0);
+      p.r_pos_stride = c.dims == 2 ? q.stride(1) : c.rows.V;
+    }
+    p.clip_low = p.clip_high = 0.2f;
+    if (given(a[8])) {
+      p.clip_low = float_attr(a[8], N->clip_low);
+      p.clip_high = float_attr(a[8], N->clip_high);
+      p.kl_coef = float_attr(a[8], N->kl_coef);
+      p.entropy_coef = float_attr(a[8], N->entropy_coef);
+    }
+    p.grad_scale = c.one(a[9], 1, "grad_scale");
+    Objects<7> out;
+    const at::IntArrayRef size(c.shape, c.dims);
+    p.loss = out.make<float>(c, {}, at::kFloat);
+    p.token_loss = out.make<float>(c, size, at::kFloat);
+    c.rows.logprob = out.make<float>(c, size, at::kFloat);
+    c.rows.entropy = out.make<float>(c, size, at::kFloat);
+    p.kl = out.make<float>(c, size, at::kFloat);
+    c.rows.status = out.make<uint32_t>(c, size, at::kInt);
+    if (truth(a[10], true)) out.add(c.gradient(a[11]));
+    else out.add(Py_NewRef(Py_None));
+    enqueue("adasd_policy_loss", [&] { return g_abi.policy_loss(&c.rows, &p, c.stream); });
+    return out.call(g_policy_result);
+  });
+}
+
+PyObject* py_preference_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  return guarded([&]() -> PyObject* {
+    static PyObject* const names[] = {intern("logits"), intern("tokens"), intern("workspace"), intern("weight"), intern("ref_logprob"),
+                                      intern("pair_weight"), intern("options"), intern("grad_scale"), intern("need_grad"), intern("dlogits")};
+    PyObject* a[10];
+    parse("preference_loss", names, 3, args, nargs, kw, a);
+    RowsCall c(a[0], a[1], a[2], true);
+    adasd_preference_args p{};
+    const int64_t P = c.shape[0] / 2;
+    c.rows.weight = (const float*)c.maybe(a[3], at::kFloat, "weight");
+    p.ref_logprob = (const float*)c.maybe(a[4], at::kFloat, "ref_logprob");
+    p.pair_weight = c.one(a[5], P, "pair_weight");
+    p.beta = 0.1f;
+    if (given(a[6])) {
+      static const char* const kinds[] = {"logistic", "squared", "hinge"};
+      Ref kind(a[6], N->kind);
+      p.kind = -1;
+      for (int i = 0; i < 3; ++i)
+        if (PyUnicode_Check(kind.o) && PyUnicode_CompareWithASCIIString(kind.o, kinds[i]) == 0) p.kind = i;
+      if (p.kind < 0) fail(PyExc_ValueError, "kind must be 'logistic', 'squared' or 'hinge'");
+      p.beta = float_attr(a[6], N->beta);
+      p.margin = float_attr(a[6], N->margin);
+      p.label_smoothing = float_attr(a[6], N->label_smoothing);
+    }
+    p.grad_scale = c.one(a[7], 1, "grad_scale");
+    Objects<7> out;
+    const at::IntArrayRef size(c.shape, 2), pairs(&P, 1), sequences(c.shape, 1);
+    p.loss = out.make<float>(c, {}, at::kFloat);
+    p.pair_loss = out.make<float>(c, pairs, at::kFloat);
+    p.pair_margin = out.make<float>(c, pairs, at::kFloat);
+    p.score = out.make<float>(c, sequences, at::kFloat);
+    c.rows.logprob = out.make<float>(c, size, at::kFloat);
+    c.rows.status = out.make<uint32_t>(c, size, at::kInt);
+    if (truth(a[8], true)) out.add(c.gradient(a[9]));
+    else out.add(Py_NewRef(Py_None));
+    enqueue("adasd_preference_loss", [&] { return g_abi.preference_loss(&c.rows, &p, c.stream); });
+    return out.call(g_preference_result);
+  });
+}
+
+// connect_losses(PolicyResult, PreferenceResult, addresses of token_logprob, token_logprob_grad, policy_loss, preference_loss)
+PyObject* py_connect_losses(PyObject*, PyObject* args) {
+  PyObject *policy, *preference;
+  unsigned long long f[4];
+  if (!PyArg_ParseTuple(args, "OOKKKK", &policy, &preference, &f[0], &f[1], &f[2], &f[3])) return nullptr;
+  Py_INCREF(policy);
+  Py_INCREF(preference);
+  Py_XSETREF(g_policy_result, policy);
+  Py_XSETREF(g_preference_result, preference);
+  g_abi.token_logprob = (decltype(g_abi.token_logprob))f[0];
+  g_abi.token_logprob_grad = (decltype(g_abi.token_logprob_grad))f[1];
+  g_abi.policy_loss = (decltype(g_abi.policy_loss))f[2];
+  g_abi.preference_loss = (decltype(g_abi.preference_loss))f[3];
+  Py_RETURN_NONE;
+}
+
 // connect(error class, result allocator, addresses of draft_entropy, draft_step, verify, verify_noalloc)
 PyObject* py_connect(PyObject*, PyObject* args) {
   PyObject *err, *alloc;
@@ -389,6 +670,11 @@ PyMethodDef methods[] = {
     {"draft_entropy", (PyCFunction)(void (*)(void))py_draft_entropy, METH_FASTCALL | METH_KEYWORDS, nullptr},
     {"draft_step", (PyCFunction)(void (*)(void))py_draft_step, METH_FASTCALL | METH_KEYWORDS, nullptr},
     {"verify", (PyCFunction)(void (*)(void))py_verify, METH_FASTCALL | METH_KEYWORDS, nullptr},
+    {"token_logprob", (PyCFunction)(void (*)(void))py_token_logprob, METH_FASTCALL | METH_KEYWORDS, nullptr},
+    {"token_logprob_grad", (PyCFunction)(void (*)(void))py_token_logprob_grad, METH_FASTCALL | METH_KEYWORDS, nullptr},
+    {"policy_loss", (PyCFunction)(void (*)(void))py_policy_loss, METH_FASTCALL | METH_KEYWORDS, nullptr},
+    {"preference_loss", (PyCFunction)(void (*)(void))py_preference_loss, METH_FASTCALL | METH_KEYWORDS, nullptr},
+    {"connect_losses", py_connect_losses, METH_VARARGS, nullptr},
     {"connect", py_connect, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

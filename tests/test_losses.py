@@ -75,14 +75,40 @@ def lib():
     import paper_2512_11280_amd as am
     from paper_2512_11280_amd import build as b
     b.build(force=False)
-    return am.load_library()
+    L = am.load_library()
+    L.adasd_token_logprob.argtypes = [C.POINTER(_Rows), C.c_void_p]
+    L.adasd_token_logprob_grad.argtypes = [C.POINTER(_Rows), C.c_void_p, C.c_void_p, C.c_void_p]
+    L.adasd_policy_loss.argtypes = [C.POINTER(_Rows), C.POINTER(_PolicyArgs), C.c_void_p]
+    L.adasd_preference_loss.argtypes = [C.POINTER(_Rows), C.POINTER(_PreferenceArgs), C.c_void_p]
+    return L
+
+
+class _Rows(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("dt", C.c_int), ("B", C.c_int32), ("T", C.c_int32), ("V", C.c_int32),
+                ("seq_stride", C.c_int64), ("pos_stride", C.c_int64), ("tokens", C.c_void_p), ("weight", C.c_void_p),
+                ("active", C.c_void_p), ("logprob", C.c_void_p), ("entropy", C.c_void_p), ("status", C.c_void_p),
+                ("dlogits", C.c_void_p), ("d_seq_stride", C.c_int64), ("d_pos_stride", C.c_int64),
+                ("workspace", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
+class _PolicyArgs(C.Structure):
+    _fields_ = [("advantage", C.c_void_p), ("adv_per_seq", C.c_int32), ("old_logprob", C.c_void_p),
+                ("ref_logprob", C.c_void_p), ("ref_logits", C.c_void_p), ("r_seq_stride", C.c_int64),
+                ("r_pos_stride", C.c_int64), ("grad_scale", C.c_void_p), ("clip_low", C.c_float), ("clip_high", C.c_float),
+                ("kl_coef", C.c_float), ("entropy_coef", C.c_float), ("loss", C.c_void_p), ("token_loss", C.c_void_p),
+                ("kl", C.c_void_p)]
+
+
+class _PreferenceArgs(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("beta", C.c_float), ("margin", C.c_float), ("label_smoothing", C.c_float),
+                ("ref_logprob", C.c_void_p), ("pair_weight", C.c_void_p), ("grad_scale", C.c_void_p), ("loss", C.c_void_p),
+                ("pair_loss", C.c_void_p), ("pair_margin", C.c_void_p), ("score", C.c_void_p)]
 
 
 P0 = 1 << 20            # addresses that are never followed: every call below is refused on the host
 
 
 def _rows(**kw):
-    from paper_2512_11280_amd.binding import _Rows
     a = _Rows(P0, 1, 2, 3, 100, 300, 100, P0 << 4)
     a.dlogits, a.d_seq_stride, a.d_pos_stride = P0 << 8, 300, 100
     a.workspace, a.ws_bytes = P0 << 10, 1 << 30
@@ -92,7 +118,6 @@ def _rows(**kw):
 
 
 def _policy(**kw):
-    from paper_2512_11280_amd.binding import _PolicyArgs
     p = _PolicyArgs(P0 << 5, 0, P0 << 5)
     p.clip_low = p.clip_high = 0.2
     p.loss = P0 << 5
@@ -103,7 +128,6 @@ def _policy(**kw):
 
 
 def _preference(**kw):
-    from paper_2512_11280_amd.binding import _PreferenceArgs
     p = _PreferenceArgs(0, 0.1, 0.0, 0.0)
     p.loss = P0 << 5
     for k, v in kw.items():
