@@ -6,26 +6,30 @@
 namespace adasd {
 
 namespace {
-constexpr size_t kPerPosition = sizeof(LossCoef) + 2 * sizeof(double) + sizeof(float) + 2 * sizeof(float4);
-constexpr size_t kLossSlack = (size_t)kMaxLossRecords * 2 * sizeof(float4) + 5 * 256;
+constexpr size_t kPerPosition = sizeof(LossCoef) + 2 * sizeof(double) + sizeof(float);
+constexpr size_t kLossFixed = (size_t)kMaxLossSlices * kXchgWords * sizeof(uint64_t) + (kTicketLossLen + 1 + kAddsUp) * sizeof(int32_t) + 7 * 256;
 }  // namespace
 
-size_t loss_workspace_bytes_for(size_t positions) { return kLossSlack + (positions + 1) * kPerPosition; }
+size_t loss_workspace_bytes_for(size_t positions) { return kLossFixed + (positions + 1) * kPerPosition; }
 
+// (Offsets depend on the size of the workspace alone, and those of the words and counters not even on that: a call of another shape finds
+// them where the one before left them, at zero.)
 size_t loss_workspace_layout(size_t ws_bytes, LossWorkspace* ws, void* base) {
-  if (ws_bytes <= kLossSlack) return 0;
-  const size_t cap = (ws_bytes - kLossSlack) / kPerPosition;
+  if (ws_bytes <= kLossFixed) return 0;
+  const size_t cap = (ws_bytes - kLossFixed) / kPerPosition;
   char* p = static_cast<char*>(base);
   auto take = [&](size_t bytes) {
     char* at = p;
     p += (bytes + 255) / 256 * 256;
     return at;
   };
+  ws->xchg = reinterpret_cast<uint64_t*>(take((size_t)kMaxLossSlices * kXchgWords * sizeof(uint64_t)));
+  ws->ticket = reinterpret_cast<int32_t*>(take(kTicketLossLen * sizeof(int32_t)));
+  ws->done = reinterpret_cast<int32_t*>(take((1 + kAddsUp) * sizeof(int32_t)));
   ws->coef = reinterpret_cast<LossCoef*>(take(cap * sizeof(LossCoef)));
   ws->term = reinterpret_cast<double*>(take(cap * sizeof(double)));
   ws->pair = reinterpret_cast<double*>(take(cap * sizeof(double)));
   ws->seq = reinterpret_cast<float*>(take(cap * sizeof(float)));
-  ws->rec = reinterpret_cast<float4*>(take((cap + kMaxLossRecords) * 2 * sizeof(float4)));
   return cap;
 }
 
@@ -118,7 +122,7 @@ int adasd_loss_workspace_bytes(int B, int T, int V, adasd_dtype dt, size_t* byte
   return ADASD_OK;
 }
 
-int adasd_token_logprob(const adasd_rows* a, void* stream) {
+static int token_logprob(const adasd_rows* a, void* stream, WordWait wait) {
   LossRows rows;
   LossWorkspace ws{};
   const int rc = loss_setup(a, nullptr, 0, 0, false, &rows, &ws);
@@ -127,8 +131,16 @@ int adasd_token_logprob(const adasd_rows* a, void* stream) {
   rows.g = RowPlace{};
   LossTerm f{};
   f.kind = kLogprob;
+  f.wait = wait;
   return run(rows, (int)a->dt, f, ws, stream);
 }
+
+int adasd_token_logprob(const adasd_rows* a, void* stream) { return token_logprob(a, stream, kWaits); }
+
+// For the tests, not part of the ABI: the same where records that are there count as not there, and where the last slice gives its
+// rows up at once.
+int adasd_test_logprob_unarrived(const adasd_rows* a, void* stream) { return token_logprob(a, stream, kNotThere); }
+int adasd_test_logprob_given_up(const adasd_rows* a, void* stream) { return token_logprob(a, stream, kGivesUp); }
 
 int adasd_token_logprob_grad(const adasd_rows* a, const float* dlogprob, const float* dentropy, void* stream) {
   LossRows rows;
@@ -139,6 +151,7 @@ int adasd_token_logprob_grad(const adasd_rows* a, const float* dlogprob, const f
   if (!dlogprob || !a->dlogits) return ADASD_ERR_INVALID_ARG;
   if (!aligned_to(dlogprob, 4) || !aligned_to(dentropy, 4)) return ADASD_ERR_MISALIGNED;
   LossTerm f{};
+  f.wait = kWaits;
   f.kind = kLogprob;
   f.dlogprob = dlogprob;
   f.dentropy = dentropy;
@@ -160,6 +173,7 @@ int adasd_policy_loss(const adasd_rows* a, const adasd_policy_args* p, void* str
       !aligned_to(p->grad_scale, 4) || !aligned_to(p->token_loss, 4) || !aligned_to(p->kl, 4))
     return ADASD_ERR_MISALIGNED;
   LossTerm f{};
+  f.wait = kWaits;
   f.kind = kPolicy;
   f.advantage = p->advantage;
   f.adv_per_seq = p->adv_per_seq;
@@ -191,6 +205,7 @@ int adasd_preference_loss(const adasd_rows* a, const adasd_preference_args* p, v
       !aligned_to(p->pair_loss, 4) || !aligned_to(p->pair_margin, 4) || !aligned_to(p->score, 4))
     return ADASD_ERR_MISALIGNED;
   LossTerm f{};
+  f.wait = kWaits;
   f.kind = kPreference;
   f.pair_kind = p->kind;
   f.P = a->B / 2;

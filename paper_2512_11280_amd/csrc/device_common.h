@@ -72,6 +72,26 @@ __device__ __forceinline__ double log2_fine(float x) {
   return (double)e + (2.0 / 0.693147180559945309417232) * f * p;
 }
 
+// e^d - 1 to about 1e-14 relative, whatever the size of d: e^d = 2^k e^r, |r| <= ln 2 / 2, and the series of e^r - 1.
+__device__ __forceinline__ double expm1_fine(double d) {
+  const double k = rint(fmin(fmax(d, -800.0), 800.0) * 1.44269504088896340736);
+  double r = fma(-k, 0x1.62e42fee00000p-1, d);                     // (ln 2 in two parts, the first with zeros at its end)
+  r = fma(-k, 0x1.a39ef35793c76p-33, r);
+  double p = 1.0 / 39916800;
+  p = fma(p, r, 1.0 / 3628800);
+  p = fma(p, r, 1.0 / 362880);
+  p = fma(p, r, 1.0 / 40320);
+  p = fma(p, r, 1.0 / 5040);
+  p = fma(p, r, 1.0 / 720);
+  p = fma(p, r, 1.0 / 120);
+  p = fma(p, r, 1.0 / 24);
+  p = fma(p, r, 1.0 / 6);
+  p = fma(p, r, 0.5);
+  p = fma(p * r, r, r);
+  const double v = k == 0.0 ? p : ldexp(p + 1.0, (int)k) - 1.0;
+  return d > 709.0 ? (double)INFINITY : d < -745.0 ? -1.0 : v;     // (NaN: neither)
+}
+
 // ---------------------------------------------------------------------------------------------
 // Issue order on gfx950, measured with one-instruction loops at eight wavefronts per SIMD.  A SIMD takes two
 // vector instructions at a time if they come from different wavefronts and at least one of them is plain
@@ -430,6 +450,9 @@ __device__ __forceinline__ void st_agent(float* p, float v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ void st_agent(int* p, int v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void st_agent(double* p, double v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ void publish_barrier() {

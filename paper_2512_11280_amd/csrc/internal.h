@@ -210,21 +210,30 @@ struct LossTerm {       // what the numbers of a position are formed from
   float* pair_loss;
   float* pair_margin;
   float* score;
+  // set by launch_loss
+  int32_t adds_up;              // the position, or pair, that is done last adds up the loss
+  WordWait wait;                // for the slices' records (see hand_off)
 };
 struct LossCoef {       // of a position: its gradient row is a 1[j = x] + 2^(x_j - m) (k0 + k1 (x_j - m) + k2 dd_j) (loss_device.h)
   float m, a, k0, k1, k2, c, pad[2];
 };
 struct LossWorkspace {
+  uint64_t* xchg;       // [kMaxLossSlices][kXchgWords] hand-off words of the slices, zero between launches
+  int32_t* ticket;      // [kTicketLossLen] arrival words of the rows cut into slices, zero between launches
+  int32_t* done;        // [1 + kAddsUp] positions (or pairs) that are done, and positions of each pair; zero between launches
   LossCoef* coef;       // [n]
   double* term;         // [n] what a position adds to the loss or to its sequence's score
   double* pair;         // [n] what a pair adds to the loss
   float* seq;           // [n] derivative of the loss by a sequence's score
-  float4* rec;          // [slices of all rows][2] sums of the slices
 };
-constexpr int kMaxLossRecords = 8 * 1792;      // slices beyond one per row (scan_split)
+constexpr int kMaxLossSlices = 8 * kResidentGroups;      // of all rows that are cut into more than one (scan_split)
+constexpr int kTicketLossLen = 32768;
+// Up to so many positions the last one done adds up the loss, which saves a launch or two (3 to 5 us); of more, that many additions to one
+// counter come one after the other, and a launch of its own is lost beside what they take.
+constexpr int kAddsUp = 4096;
 size_t loss_workspace_bytes_for(size_t positions);
 size_t loss_workspace_layout(size_t ws_bytes, LossWorkspace* ws, void* base);
-hipError_t launch_loss(const LossRows& rows, int dt, const LossTerm& term, const LossWorkspace& ws, hipStream_t st);
+hipError_t launch_loss(const LossRows& rows, int dt, LossTerm term, const LossWorkspace& ws, hipStream_t st);
 
 // plain streaming read (diagnostics): one word per workgroup goes to `sink`
 size_t stream_read_groups(size_t bytes);

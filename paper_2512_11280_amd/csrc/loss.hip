@@ -1,19 +1,22 @@
 // Log-probabilities of tokens, the clipped policy loss and the preference loss over vocabulary rows, with their gradients.
 //
 // A gradient row needs the row's normaliser (and entropy, and KL) before its first element, and the preference loss those of whole
-// sequences: the rows are read, the few numbers of each position settled, and the rows read again for the gradient.
-//   k_loss_sums  (slices of rows)  -> sums of each slice (loss_device.h)
-//   k_loss_rows  (a wavefront per position) folds the slices, writes what is reported of the position, and the five numbers of its
-//                gradient row
-//   k_loss_pairs (a workgroup per pair; preference only) the scores of the two sequences, the pair's loss and slope
-//   k_loss_grad  (slices of rows)  -> the gradient
-//   k_loss_total (one workgroup)   adds up the loss
-// Sums over positions and sequences are in 64 bits and in a fixed order.
+// sequences.
+//   k_loss_sums  (slices of rows) the sums of each slice (loss_device.h).  One workgroup of a row folds them (hand_off), settles the
+//                position: what is reported of it, and the five numbers of its gradient row.  The position that is done last adds up
+//                the loss; of a pair's sequences, settles the pair.
+//   k_loss_grad  (slices of rows) reads the logits again and forms the gradient.
+//   k_loss_fused (a workgroup per row, which stays in registers) both in one, where the gradient needs nothing but its own row.
+//   k_loss_pairs, k_loss_total: pairs and the sum of the loss where there are many positions.
+// Sums over positions and sequences are in 64 bits and in a fixed order, whoever forms them.
 #include "loss_device.h"
+#include "sample_device.h"
 
 namespace adasd {
 
 namespace {
+
+using namespace sampling;
 
 // Vectors v0 .. v1 of a row that slice s of S works on.
 __device__ __forceinline__ void slice_of(int nv, int s, int S, int& v0, int& v1) {
@@ -32,52 +35,47 @@ template <int DT> __device__ __forceinline__ float ref_shift(const char* row, co
   return fabsf(d) < INFINITY ? d : 0.f;
 }
 
-template <int DT, bool REF> __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, int S, float4* rec) {
-  __shared__ LossSums sh[kWaves];
-  const int r = blockIdx.x, s = blockIdx.y, tid = threadIdx.x;
-  if (!position_counts(rows, r)) return;
-  const int b = r / rows.T, t = r - b * rows.T, V = rows.V;
-  const char* row = row_at<DT>(rows.z, b, t);
-  const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
-  const float c = REF ? ref_shift<DT>(row, ref, rows.tokens[r], V) : 0.f;
-  int v0, v1;
-  slice_of(vectors_of<DT>(V), s, S, v0, v1);
-  LossSums a = loss_empty();
-  for (int idx = v0 + tid; idx < v1; idx += kBlock) {
-    const uint4 x = load_vec_of<DT>(row, idx, V);
-    loss_push<DT, REF>(a, x, REF ? load_vec_of<DT>(ref, idx, V) : x, c);
+// What the numbers of a position are formed from, asked for ahead of the row.
+struct PositionIn {
+  float z, weight, a, h, old, ref;      // logit of the token; a: advantage or dlogprob; h: dentropy
+  int x;
+};
+__device__ __forceinline__ PositionIn ask_position(const LossRows& rows, const LossTerm& f, int r, int b) {
+  PositionIn in{};
+  in.x = rows.tokens[r];
+  in.weight = rows.weight ? rows.weight[r] : 1.f;
+  if (f.kind == kLogprob) {
+    if (f.dlogprob) in.a = f.dlogprob[r];
+    if (f.dentropy) in.h = f.dentropy[r];
+  } else {
+    if (f.kind == kPolicy) in.a = f.advantage[f.adv_per_seq ? b : r];
+    if (f.old_logprob) in.old = f.old_logprob[r];
+    if (f.ref_logprob) in.ref = f.ref_logprob[r];
   }
-  a = loss_fold_wave<REF>(a);
-  if ((tid & 63) == 0) sh[tid >> 6] = a;
-  __syncthreads();
-  if (tid < 64) {
-    a = tid < kWaves ? sh[tid] : loss_empty();
-    a = loss_fold_wave<REF>(a);
-    if (tid == 0) {
-      rec[2 * ((size_t)r * S + s)] = make_float4(a.m, a.s, a.u, a.w);
-      rec[2 * ((size_t)r * S + s) + 1] = make_float4(a.mr, a.sr, c, 0.f);
-    }
-  }
+  return in;
+}
+template <int DT> __device__ __forceinline__ void ask_logit(PositionIn& in, const char* row, int V) {
+  in.z = load_elem<DT>(row, in.x >= 0 && in.x < V ? in.x : 0);
 }
 
-// What is reported of a position, and the numbers of its gradient row (from the sums of the whole row).
-template <int DT, bool REF>
-__device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const LossTerm& f, int r, const LossSums& sums, float c,
-                                                    double& term) {
-  const int b = r / rows.T, t = r - b * rows.T, x = rows.tokens[r];
-  const bool known = x >= 0 && x < rows.V;
+// What is reported of a position (lane 0 writes it), and the numbers of its gradient row, by one wavefront from the sums of the whole row.
+template <bool REF>
+__device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const LossTerm& f, int r, const PositionIn& in, const LossSums& sums,
+                                                    float c, double& term) {
+  const int lane = threadIdx.x & 63;
+  const bool known = in.x >= 0 && in.x < rows.V;
   const LossRow row = finish_loss_row<REF>(sums, c);
-  const double lp = known ? (double)load_elem<DT>(row_at<DT>(rows.z, b, t), known ? x : 0) - row.lse : (double)NAN;
-  const double w = rows.weight ? (double)rows.weight[r] : 1.0;
-  double a = 0.0, by_entropy = 0.0, by_kl = 0.0;
+  const double lp = known ? (double)in.z - row.lse : (double)NAN;
+  const double w = (double)in.weight;
+  double a = 0.0, by_entropy = 0.0, by_kl = 0.0, loss = 0.0, kl = row.kl;
   term = 0.0;
   if (f.kind == kLogprob) {
-    if (f.dlogprob) a = (double)f.dlogprob[r];
-    if (f.dentropy) by_entropy = (double)f.dentropy[r];
+    a = (double)in.a;
+    by_entropy = (double)in.h;
   } else if (f.kind == kPolicy) {
-    const double A = (double)f.advantage[f.adv_per_seq ? b : r];
-    const double ratio = f.old_logprob ? exp(lp - (double)f.old_logprob[r]) : lp == lp ? 1.0 : lp;
-    double loss = 0.0, kl = row.kl;
+    // one exponential for both ratios: the old policy's in the even lanes, the reference's in the odd ones
+    const double grown = expm1_fine(lane & 1 ? (double)in.ref - lp : lp - (double)in.old);
+    const double A = (double)in.a, ratio = f.old_logprob ? 1.0 + __shfl(grown, 0) : lp == lp ? 1.0 : lp, grown_ref = __shfl(grown, 1);
     if (A != 0.0) {
       const double free = ratio * A, held = fmin(fmax(ratio, 1.0 - (double)f.clip_low), 1.0 + (double)f.clip_high) * A;
       const bool clipped = held < free;
@@ -85,105 +83,78 @@ __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const 
       a = clipped ? 0.0 : -free;
     }
     if (f.ref_logprob) {
-      const double d = (double)f.ref_logprob[r] - lp, grown = expm1(d);
-      kl = grown - d;
-      if (f.kl_coef != 0.f) a -= (double)f.kl_coef * grown;
+      kl = grown_ref - ((double)in.ref - lp);
+      if (f.kl_coef != 0.f) a -= (double)f.kl_coef * grown_ref;
     }
     if (f.kl_coef != 0.f) loss += (double)f.kl_coef * kl;
     if (f.entropy_coef != 0.f) loss -= (double)f.entropy_coef * row.H;
     term = w * loss;
-    if (f.token_loss) f.token_loss[r] = (float)loss;
-    if (f.kl) f.kl[r] = (float)kl;
     const double scale = w * (f.grad_scale ? (double)*f.grad_scale : 1.0);
     a *= scale;
     by_entropy = -scale * (double)f.entropy_coef;
     if (REF) by_kl = scale * (double)f.kl_coef;
   } else {
-    term = w * (lp - (f.ref_logprob ? (double)f.ref_logprob[r] : 0.0));
+    term = w * (lp - (f.ref_logprob ? (double)in.ref : 0.0));
     a = w;
   }
-  if (rows.logprob) rows.logprob[r] = (float)lp;
-  if (rows.entropy) rows.entropy[r] = (float)row.H;
-  if (rows.status) rows.status[r] = (known ? 0u : (uint32_t)ADASD_ST_BAD_TOKEN) | (row.bad ? (uint32_t)ADASD_ST_NONFINITE : 0u);
+  if (lane == 0) {
+    if (rows.logprob) rows.logprob[r] = (float)lp;
+    if (rows.entropy) rows.entropy[r] = (float)row.H;
+    if (rows.status) rows.status[r] = (known ? 0u : (uint32_t)ADASD_ST_BAD_TOKEN) | (row.bad ? (uint32_t)ADASD_ST_NONFINITE : 0u);
+    if (f.token_loss) f.token_loss[r] = (float)loss;
+    if (f.kl) f.kl[r] = (float)kl;
+  }
   // dz_j = a (1[j = x] - p_j) - by_entropy p_j (ln p_j + H) + by_kl p_j (ln p_j - ln q_j - KL)
   LossCoef k{};
-  const double inv_s = (double)row.inv_s;
   double k0 = -a;
   if (by_entropy != 0.0) {
     k0 -= by_entropy * (row.H - (row.lse - kNat * (double)sums.m));
-    k.k1 = (float)(-by_entropy * kNat * inv_s);
+    k.k1 = (float)(-by_entropy * kNat * row.inv_s);
   }
   if (REF && by_kl != 0.0) {
     k0 += by_kl * (kNat * (double)c - (row.lse - row.lse_ref) - row.kl);
-    k.k2 = (float)(by_kl * kNat * inv_s);
+    k.k2 = (float)(by_kl * kNat * row.inv_s);
   }
   k.m = sums.m;
   k.c = c;
   k.a = (float)a;
-  k.k0 = k0 == 0.0 ? 0.f : (float)(k0 * inv_s);      // (nothing of the row enters a gradient of zeros)
+  k.k0 = k0 == 0.0 ? 0.f : (float)(k0 * row.inv_s);      // (nothing of the row enters a gradient of zeros)
   return k;
 }
 
 // The results of a position that does not count.
-__device__ __forceinline__ void report_nothing(const LossRows& rows, const LossTerm& f, const LossWorkspace& ws, int r) {
+__device__ __forceinline__ void report_nothing(const LossRows& rows, const LossTerm& f, int r) {
   if (rows.logprob) rows.logprob[r] = 0.f;
   if (rows.entropy) rows.entropy[r] = 0.f;
   if (rows.status) rows.status[r] = 0u;
   if (f.token_loss) f.token_loss[r] = 0.f;
   if (f.kl) f.kl[r] = 0.f;
-  ws.term[r] = 0.0;
 }
 
-template <int DT, bool REF> __global__ void __launch_bounds__(kBlock) k_loss_rows(LossRows rows, LossTerm f, int S, LossWorkspace ws) {
-  const int r = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (r >= rows.n) return;
-  if (!position_counts(rows, r)) {
-    if (lane == 0) {
-      report_nothing(rows, f, ws, r);
-      ws.coef[r] = LossCoef{};
-    }
-    return;
-  }
-  LossSums a = loss_empty();
-  float c = 0.f;
-  if (REF) c = ws.rec[2 * (size_t)r * S + 1].z;
-  if (lane < S) {
-    const float4 p = ws.rec[2 * ((size_t)r * S + lane)], q = ws.rec[2 * ((size_t)r * S + lane) + 1];
-    a = LossSums{p.x, p.y, p.z, p.w, q.x, q.y};
-  }
-  a = loss_fold_wave<REF>(a);
-  if (lane == 0) {
-    double term;
-    ws.coef[r] = settle_position<DT, REF>(rows, f, r, a, c, term);
-    ws.term[r] = term;
-  }
-}
-
-// Sum of v over the workgroup in 64 bits, in thread 0 (a fixed order).
-__device__ __forceinline__ double block_sum(double v, double (&sh)[kWaves]) {
-  v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-  __syncthreads();
+// ---- sums over positions.  One wavefront; the order of the additions is the same whether other workgroups' terms are read in the launch
+// that forms them (FRESH) or in a later one.
+template <bool FRESH> __device__ __forceinline__ double wave_total(const double* v, int n) {
+  const int lane = threadIdx.x & 63;
   double t = 0.0;
+  for (int base = 0; base < n; base += 8 * 64) {
+    double x[8];
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) t += sh[w];
-  return t;
-}
-__device__ __forceinline__ double strided_sum(const double* v, int n) {
-  double t = 0.0;
-  for (int i = threadIdx.x; i < n; i += kBlock) t += v[i];
-  return t;
+    for (int k = 0; k < 8; ++k) {
+      const int i = base + k * 64 + lane;
+      x[k] = i < n ? (FRESH ? ld_agent(v + i) : v[i]) : 0.0;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t += x[k];
+  }
+  return wave_sum(t);
 }
 
 __device__ __forceinline__ double softplus(double v) { return fmax(v, 0.0) + log1p(exp(-fabs(v))); }
 
-__global__ void __launch_bounds__(kBlock) k_loss_pairs(LossTerm f, int T, LossWorkspace ws) {
-  __shared__ double sh[kWaves];
-  const int i = blockIdx.x, P = f.P;
-  const double chosen = block_sum(strided_sum(ws.term + (size_t)i * T, T), sh);
-  const double rejected = block_sum(strided_sum(ws.term + (size_t)(P + i) * T, T), sh);
-  if (threadIdx.x != 0) return;
+// A pair's loss and slope from the terms of its positions, by one wavefront (lane 0 writes).
+template <bool FRESH> __device__ __forceinline__ void settle_pair(const LossTerm& f, const LossWorkspace& ws, int i, int T) {
+  const int P = f.P;
+  const double chosen = wave_total<FRESH>(ws.term + (size_t)i * T, T), rejected = wave_total<FRESH>(ws.term + (size_t)(P + i) * T, T);
   const double beta = (double)f.beta, e = (double)f.smoothing, D = chosen - rejected;
   double m, loss, slope;
   if (f.pair_kind == 1) {
@@ -196,17 +167,17 @@ __global__ void __launch_bounds__(kBlock) k_loss_pairs(LossTerm f, int T, LossWo
     if (f.pair_kind == 2) {
       loss = fmax(1.0 - m, 0.0);
       slope = m < 1.0 ? -beta : 0.0;
-      if (m != m) loss = slope = m;
     } else {
       // (a part with factor 0 is left out: its logarithm may be infinite)
       loss = (e < 1.0 ? (1.0 - e) * softplus(-m) : 0.0) + (e > 0.0 ? e * softplus(m) : 0.0);
       slope = beta * (e / (1.0 + exp(-m)) - (1.0 - e) / (1.0 + exp(m)));
-      if (m != m) loss = slope = m;
     }
+    if (m != m) loss = slope = m;
   }
   const double w = f.pair_weight ? (double)f.pair_weight[i] : 1.0 / (double)P;
   const double scale = w * (f.grad_scale ? (double)*f.grad_scale : 1.0);
-  ws.pair[i] = w != 0.0 ? w * loss : 0.0;
+  if ((threadIdx.x & 63) != 0) return;
+  st_agent(ws.pair + i, w != 0.0 ? w * loss : 0.0);
   ws.seq[i] = w != 0.0 ? (float)(scale * slope) : 0.f;
   ws.seq[P + i] = w != 0.0 ? (float)(-scale * slope) : 0.f;
   if (f.pair_loss) f.pair_loss[i] = (float)loss;
@@ -217,9 +188,123 @@ __global__ void __launch_bounds__(kBlock) k_loss_pairs(LossTerm f, int T, LossWo
   }
 }
 
-__global__ void __launch_bounds__(kBlock) k_loss_total(const double* v, int n, float* out) {
-  __shared__ double sh[kWaves];
-  const double t = block_sum(strided_sum(v, n), sh);
+// Whether this is the last of n to come to a counter, which is zero again then: all that the others stored before is to be read.
+__device__ __forceinline__ bool last_of(int32_t* counter, int n) {
+  stores_before_loads();
+  if (!last_to_add(add_arrival(counter), n)) return false;
+  set_arrival(counter, 0);
+  return true;
+}
+// Position r is settled (one wavefront): the last of a pair settles the pair, the last of all adds up the loss.
+__device__ __forceinline__ void position_done(const LossRows& rows, const LossTerm& f, const LossWorkspace& ws, int r, double term) {
+  if (!f.loss) return;
+  if ((threadIdx.x & 63) == 0) st_agent(ws.term + r, term);
+  if (!f.adds_up) return;
+  int n = rows.n;
+  const double* v = ws.term;
+  if (f.kind == kPreference) {
+    const int b = r / rows.T, i = b < f.P ? b : b - f.P;
+    if (!last_of(ws.done + 1 + i * ticket_stride(f.P, kAddsUp), 2 * rows.T)) return;
+    settle_pair<true>(f, ws, i, rows.T);
+    n = f.P;
+    v = ws.pair;
+  }
+  if (!last_of(ws.done, n)) return;
+  const double t = wave_total<true>(v, n);
+  if ((threadIdx.x & 63) == 0) *f.loss = (float)t;
+}
+
+// Sums of a whole row by one wavefront (where the slices' records did not arrive, which never happens to calls that are ordered as they
+// have to be).
+template <int DT, bool REF> __device__ __noinline__ LossSums wave_row_sums(const char* row, const char* ref, int V, float c) {
+  LossSums a = loss_empty();
+#pragma unroll 1
+  for (int idx = threadIdx.x & 63; idx < vectors_of<DT>(V); idx += 64) {
+    const uint4 x = load_vec_of<DT>(row, idx, V);
+    loss_push<DT, REF>(a, x, REF ? load_vec_of<DT>(ref, idx, V) : x, c);
+  }
+  return loss_fold_wave<REF>(a);
+}
+
+// A slice's vectors come in batches of four per thread, the next batch on its way.
+constexpr int kSumsBatch = 4;
+template <int DT, bool REF> __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f, int S, int chunk, LossWorkspace ws) {
+  __shared__ LossSums sh[kWaves];
+  const int r = blockIdx.x / S, s = blockIdx.x - r * S, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int b = r / rows.T, t = r - b * rows.T, V = rows.V;
+  if (!position_counts(rows, r)) {
+    if (s != 0 || wave != 0) return;
+    if (lane == 0) {
+      report_nothing(rows, f, r);
+      ws.coef[r] = LossCoef{};
+    }
+    position_done(rows, f, ws, r, 0.0);
+    return;
+  }
+  PositionIn in = ask_position(rows, f, r, b);
+  const char* row = row_at<DT>(rows.z, b, t);
+  const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
+  const int nv = vectors_of<DT>(V), v0 = min(s * chunk, nv), v1 = min(v0 + chunk, nv);
+  auto load = [&](const char* from, int idx) { return idx < v1 ? load_vec_of<DT>(from, idx, V) : neutral_vec<DT>(); };
+  uint4 next[kSumsBatch], nextr[kSumsBatch];
+#pragma unroll
+  for (int k = 0; k < kSumsBatch; ++k) next[k] = load(row, v0 + tid + k * kBlock);
+  if (REF) {
+#pragma unroll
+    for (int k = 0; k < kSumsBatch; ++k) nextr[k] = load(ref, v0 + tid + k * kBlock);
+  }
+  ask_logit<DT>(in, row, V);
+  const float c = REF ? ref_shift<DT>(row, ref, in.x, V) : 0.f;
+  LossSums a = loss_empty();
+  for (int base = v0; base < v1; base += kSumsBatch * kBlock) {
+    uint4 x[kSumsBatch], xr[kSumsBatch];
+#pragma unroll
+    for (int k = 0; k < kSumsBatch; ++k) {
+      x[k] = next[k];
+      if (REF) xr[k] = nextr[k];
+    }
+    if (base + kSumsBatch * kBlock < v1) {
+#pragma unroll
+      for (int k = 0; k < kSumsBatch; ++k) {
+        const int idx = base + tid + (k + kSumsBatch) * kBlock;
+        next[k] = load(row, idx);
+        if (REF) nextr[k] = load(ref, idx);
+      }
+    }
+    loss_raise(a, vecs_max<DT, kSumsBatch>(x));
+#pragma unroll
+    for (int k = 0; k < kSumsBatch; ++k)
+      if (base + k * kBlock < v1) loss_push_at<DT, REF>(a, x[k], REF ? xr[k] : x[k], c);
+  }
+  a = loss_fold_wave<REF>(a);
+  if (lane == 0) sh[wave] = a;
+  __syncthreads();
+  if (wave != 0) return;
+  a = loss_fold_wave<REF>(lane < kWaves ? sh[lane] : loss_empty());
+  if (S > 1) {
+    uint64_t w[kXchgWords];
+    bool arrived = true;
+    pack_pair(PairRecord{a.m, a.s, a.u, REF ? a.mr : a.m, REF ? a.sr : 0.f, REF ? a.w : 0.f}, w);
+    if (!hand_off(PlainWords{ws.xchg + (size_t)r * S * kXchgWords}, s, S, Arrivals{ws.ticket, kTicketLossLen, r, rows.n}, f.wait, [] {}, w, arrived))
+      return;
+    a = loss_empty();
+    if (lane < S) {
+      const PairRecord p = unpack_pair(w);
+      a = LossSums{p.mp, p.sp, p.up, p.uq, p.mq, p.sq};
+    }
+    a = loss_fold_wave<REF>(a);
+    if (__builtin_expect(!arrived, 0)) a = wave_row_sums<DT, REF>(row, ref, V, c);
+  }
+  double term;
+  const LossCoef k = settle_position<REF>(rows, f, r, in, a, c, term);
+  if (lane == 0) ws.coef[r] = k;
+  position_done(rows, f, ws, r, term);
+}
+
+__global__ void __launch_bounds__(64) k_loss_pairs(LossTerm f, int T, LossWorkspace ws) { settle_pair<false>(f, ws, blockIdx.x, T); }
+
+__global__ void __launch_bounds__(64) k_loss_total(const double* v, int n, float* out) {
+  const double t = wave_total<false>(v, n);
   if (threadIdx.x == 0) *out = (float)t;
 }
 
@@ -284,7 +369,7 @@ __device__ __forceinline__ void grad_vec(const uint4& x, const uint4& xr, const 
 }
 
 template <int DT, bool ENT, bool REF>
-__global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int S, LossWorkspace ws, int by_sequence, const float* grad_scale) {
+__global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int S, LossWorkspace ws, int by_sequence) {
   constexpr int EPV = Elem<DT>::per_vec;
   const int r = blockIdx.x, b = r / rows.T, t = r - b * rows.T, V = rows.V;
   LossCoef k = scalar_load(ws.coef + r);
@@ -318,14 +403,16 @@ __global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int S, Loss
   }
 }
 
-// ---- Many rows: one workgroup per row, which stays in its registers (T threads, up to NB vectors each, raw) from the load to the
-// gradient: the logits are read once.
+// ---- Many rows: one workgroup of T threads per row.  The row's first NB vectors per thread stay in registers (raw) from the load to
+// the gradient, so that they are read once; what is longer, and the reference's row, is read again (from the cache behind the L2s,
+// where the few hundred rows in work fit).
 template <int W> struct FusedLoss {
   LossSums sums[W];
   LossCoef coef;
 };
-template <int DT, bool ENT, int T, int NB>
-__global__ void __launch_bounds__(T) k_loss_fused(LossRows rows, LossTerm f, LossWorkspace ws) {
+constexpr int kRefAhead = 4;      // vectors of the reference's row on their way
+template <int DT, bool ENT, bool REF, int T, int NB>
+__global__ void __launch_bounds__(T, 4) k_loss_fused(LossRows rows, LossTerm f, LossWorkspace ws) {
   constexpr int EPV = Elem<DT>::per_vec, W = T / 64;
   __shared__ FusedLoss<W> sh;
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = rows.V, whole = V / EPV, nv = vectors_of<DT>(V);
@@ -338,100 +425,125 @@ __global__ void __launch_bounds__(T) k_loss_fused(LossRows rows, LossTerm f, Los
     for (int idx = tid; idx < nv; idx += T) store_grad<DT>(out, idx, V, g);
   };
   if (!position_counts(rows, r)) {
-    if (tid == 0) report_nothing(rows, f, ws, r);
+    if (tid == 0) report_nothing(rows, f, r);
     zeros();
+    if (wave == 0) position_done(rows, f, ws, r, 0.0);
     return;
   }
+  PositionIn in = ask_position(rows, f, r, b);
   const char* row = row_at<DT>(rows.z, b, t);
-  uint4 v[NB];
-#pragma unroll
-  for (int j = 0; j < NB; ++j) {
+  const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
+  auto load = [&](const char* from, int j) {
     const int idx = tid + j * T;
-    if ((j + 1) * T <= whole) v[j] = load_vec_any(row, idx);
-    else if (idx < nv) v[j] = load_vec_of<DT>(row, idx, V);
-    else v[j] = neutral_vec<DT>();
+    if ((j + 1) * T <= whole) return load_vec_any(from, idx);
+    return idx < nv ? load_vec_of<DT>(from, idx, V) : neutral_vec<DT>();
+  };
+  uint4 v[NB], q[kRefAhead];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) v[j] = load(row, j);
+  if (REF) {
+#pragma unroll
+    for (int j = 0; j < kRefAhead; ++j) q[j] = load(ref, j);
   }
+  ask_logit<DT>(in, row, V);
+  const float c = REF ? ref_shift<DT>(row, ref, in.x, V) : 0.f;
   LossSums a = loss_empty();
   a.m = vecs_max<DT, NB>(v);
 #pragma unroll
-  for (int j = 0; j < NB; ++j)
-    if (j * T < nv) loss_push_at<DT, false>(a, v[j], v[j], 0.f);
-  a = loss_fold_wave<false>(a);
+  for (int j = 0; j < NB; ++j) {
+    if (j * T < nv) loss_push_at<DT, REF>(a, v[j], REF ? q[j % kRefAhead] : v[j], c);
+    if (REF && j + kRefAhead < NB) q[j % kRefAhead] = load(ref, j + kRefAhead);
+  }
+  for (int idx = tid + NB * T; idx < nv; idx += T) {
+    const uint4 x = load_vec_of<DT>(row, idx, V);
+    loss_push<DT, REF>(a, x, REF ? load_vec_of<DT>(ref, idx, V) : x, c);
+  }
+  a = loss_fold_wave<REF>(a);
   if (lane == 0) sh.sums[wave] = a;
   __syncthreads();
+  double term = 0.0;
   if (wave == 0) {
-    a = loss_fold_wave<false>(lane < W ? sh.sums[lane] : loss_empty());
-    if (lane == 0) {
-      double term;
-      sh.coef = settle_position<DT, false>(rows, f, r, a, 0.f, term);
-      if (f.loss) ws.term[r] = term;
-    }
+    a = loss_fold_wave<REF>(lane < W ? sh.sums[lane] : loss_empty());
+    const LossCoef mine = settle_position<REF>(rows, f, r, in, a, c, term);
+    if (lane == 0) sh.coef = mine;
+  }
+  if (REF) {
+#pragma unroll
+    for (int j = 0; j < kRefAhead; ++j) q[j] = load(ref, j);
   }
   __syncthreads();
   const LossCoef k = sh.coef;
-  if (k.a == 0.f && k.k0 == 0.f && k.k1 == 0.f) {
+  if (k.a == 0.f && k.k0 == 0.f && k.k1 == 0.f && k.k2 == 0.f) {
     zeros();
+    if (wave == 0) position_done(rows, f, ws, r, term);
     return;
   }
-  const int x = rows.tokens[r];
+  const int x = in.x;
+  auto emit = [&](int idx, const uint4& z, const uint4& zr) {
+    grad_vec<DT, ENT, REF>(z, zr, k, g);
+    if (idx == x / EPV) {
+#pragma unroll
+      for (int i = 0; i < EPV; ++i) g[i] += idx * EPV + i == x ? k.a : 0.f;
+    }
+    store_grad<DT>(out, idx, V, g);
+  };
 #pragma unroll
   for (int j = 0; j < NB; ++j) {
     const int idx = tid + j * T;
-    if (idx < nv) {
-      grad_vec<DT, ENT, false>(v[j], v[j], k, g);
-      if (idx == x / EPV) {
-#pragma unroll
-        for (int i = 0; i < EPV; ++i) g[i] += idx * EPV + i == x ? k.a : 0.f;
-      }
-      store_grad<DT>(out, idx, V, g);
-    }
+    if (idx < nv) emit(idx, v[j], REF ? q[j % kRefAhead] : v[j]);
+    if (REF && j + kRefAhead < NB) q[j % kRefAhead] = load(ref, j + kRefAhead);
   }
+  for (int idx = tid + NB * T; idx < nv; idx += T) {
+    const uint4 z = load_vec_of<DT>(row, idx, V);
+    emit(idx, z, REF ? load_vec_of<DT>(ref, idx, V) : z);
+  }
+  if (wave == 0) position_done(rows, f, ws, r, term);
 }
 
 }  // namespace
 
-hipError_t launch_loss(const LossRows& rows, int dt, const LossTerm& f, const LossWorkspace& ws, hipStream_t st) {
+hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorkspace& ws, hipStream_t st) {
   const int n = rows.n, epv = dt == ADASD_BF16 ? 8 : 4, nv = (rows.V + epv - 1) / epv;
-  const bool ref = rows.ref.base != nullptr;
+  const bool ref = rows.ref.base != nullptr, ent = f.kind == kPolicy ? f.entropy_coef != 0.f : f.kind == kLogprob && f.dentropy;
+  const bool by_ref = ref && f.kl_coef != 0.f;
+  const bool fused = rows.g.base && f.kind != kPreference && ref == by_ref && n >= 256;
   const dim3 block(kBlock);
-  const bool ent = f.kind == kPolicy ? f.entropy_coef != 0.f : f.kind == kLogprob && f.dentropy;
-  const bool fused = rows.g.base && f.kind != kPreference && !ref && n >= 256 && nv <= 1024 * 20;
+  f.adds_up = f.loss && n > 0 && n <= kAddsUp;
   if (fused) {
-    const int NB = nv <= 1024 * 16 ? 16 : 20, T = NB == 20 ? 1024 : nv <= 128 * 16 ? 128 : nv <= 256 * 16 ? 256 : nv <= 512 * 16 ? 512 : 1024;
-#define ADASD_FUSED_CASE(DTV, ENTV, TV, NBV) \
-    if (dt == DTV && ent == ENTV && T == TV && NB == NBV) launch_kernel((k_loss_fused<DTV, ENTV, TV, NBV>), dim3(n), dim3(TV), st, rows, f, ws);
-#define ADASD_FUSED_CASES(TV, NBV) ADASD_FUSED_CASE(ADASD_BF16, false, TV, NBV) ADASD_FUSED_CASE(ADASD_BF16, true, TV, NBV) \
-    ADASD_FUSED_CASE(ADASD_F32, false, TV, NBV) ADASD_FUSED_CASE(ADASD_F32, true, TV, NBV)
-    ADASD_FUSED_CASES(128, 16) ADASD_FUSED_CASES(256, 16) ADASD_FUSED_CASES(512, 16) ADASD_FUSED_CASES(1024, 16) ADASD_FUSED_CASES(1024, 20)
+    const int T = nv <= 128 * 16 ? 128 : nv <= 256 * 16 ? 256 : nv <= 512 * 16 ? 512 : 1024;
+#define ADASD_FUSED_CASE(DTV, ENTV, REFV, TV, NBV) \
+    if (dt == DTV && ent == ENTV && ref == REFV && T == TV) \
+      launch_kernel((k_loss_fused<DTV, ENTV, REFV, TV, NBV>), dim3(n), dim3(TV), st, rows, f, ws);
+#define ADASD_FUSED_CASES(TV, NBV) \
+    ADASD_FUSED_CASE(ADASD_BF16, false, false, TV, NBV) ADASD_FUSED_CASE(ADASD_BF16, true, false, TV, NBV) \
+    ADASD_FUSED_CASE(ADASD_F32, false, false, TV, NBV) ADASD_FUSED_CASE(ADASD_F32, true, false, TV, NBV) \
+    ADASD_FUSED_CASE(ADASD_BF16, false, true, TV, NBV) ADASD_FUSED_CASE(ADASD_BF16, true, true, TV, NBV) \
+    ADASD_FUSED_CASE(ADASD_F32, false, true, TV, NBV) ADASD_FUSED_CASE(ADASD_F32, true, true, TV, NBV)
+    ADASD_FUSED_CASES(128, 16) ADASD_FUSED_CASES(256, 16) ADASD_FUSED_CASES(512, 16) ADASD_FUSED_CASES(1024, 16)
 #undef ADASD_FUSED_CASES
 #undef ADASD_FUSED_CASE
   } else if (n > 0) {
-    const int S = scan_split(n, rows.V, dt);
-    const dim3 grid(n, S), waves((n + kWaves - 1) / kWaves);
+    const int S = scan_split(n, rows.V, dt), chunk = slice_chunk(nv, S);
 #define ADASD_LOSS_CASE(DTV, REFV) \
-    if (dt == DTV && ref == REFV) { \
-      launch_kernel((k_loss_sums<DTV, REFV>), grid, block, st, rows, S, ws.rec); \
-      launch_kernel((k_loss_rows<DTV, REFV>), waves, block, st, rows, f, S, ws); \
-    }
+    if (dt == DTV && ref == REFV) launch_kernel((k_loss_sums<DTV, REFV>), dim3(n * S), block, st, rows, f, S, chunk, ws);
     ADASD_LOSS_CASE(ADASD_BF16, false) ADASD_LOSS_CASE(ADASD_BF16, true) ADASD_LOSS_CASE(ADASD_F32, false) ADASD_LOSS_CASE(ADASD_F32, true)
 #undef ADASD_LOSS_CASE
-    if (f.kind == kPreference) launch_kernel(k_loss_pairs, dim3(f.P), block, st, f, rows.T, ws);
+    if (f.kind == kPreference && !f.adds_up) launch_kernel(k_loss_pairs, dim3(f.P), dim3(64), st, f, rows.T, ws);
     if (rows.g.base) {
       const int turns = 8, slices = (nv + turns * kBlock - 1) / (turns * kBlock);
       const dim3 pieces(n, slices);
-      const bool by_ref = ref && f.kl_coef != 0.f;
 #define ADASD_GRAD_CASE(DTV, ENTV, REFV) \
       if (dt == DTV && ent == ENTV && by_ref == REFV) \
-        launch_kernel((k_loss_grad<DTV, ENTV, REFV>), pieces, block, st, rows, slices, ws, f.kind == kPreference ? 1 : 0, f.grad_scale);
+        launch_kernel((k_loss_grad<DTV, ENTV, REFV>), pieces, block, st, rows, slices, ws, f.kind == kPreference ? 1 : 0);
       ADASD_GRAD_CASE(ADASD_BF16, false, false) ADASD_GRAD_CASE(ADASD_BF16, false, true) ADASD_GRAD_CASE(ADASD_BF16, true, false)
       ADASD_GRAD_CASE(ADASD_BF16, true, true) ADASD_GRAD_CASE(ADASD_F32, false, false) ADASD_GRAD_CASE(ADASD_F32, false, true)
       ADASD_GRAD_CASE(ADASD_F32, true, false) ADASD_GRAD_CASE(ADASD_F32, true, true)
 #undef ADASD_GRAD_CASE
     }
   }
-  if (f.loss) {
+  if (f.loss && !f.adds_up) {
     const bool pairs = f.kind == kPreference;
-    launch_kernel(k_loss_total, dim3(1), block, st, (const double*)(pairs ? ws.pair : ws.term), n == 0 ? 0 : pairs ? f.P : n, f.loss);
+    launch_kernel(k_loss_total, dim3(1), dim3(64), st, (const double*)(pairs ? ws.pair : ws.term), n == 0 ? 0 : pairs ? f.P : n, f.loss);
   }
   return hipGetLastError();
 }

@@ -19,12 +19,19 @@ struct LossSums {          // of a slice
 };
 __device__ __forceinline__ LossSums loss_empty() { return LossSums{kNegHuge, 0.f, 0.f, 0.f, kNegHuge, 0.f}; }
 
-// One vector of the row (and of the reference's) joins a lane's sums, about the references the sums have.  The vector's sums are
+// One vector of the row (and of the reference's) joins a lane's sums, about the reference m that the sums have (mr follows).  The vector's sums are
 // formed on their own, so that a chain of additions is one per vector long.
 template <int DT, bool REF>
 __device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const uint4& xr, float c) {
   constexpr int EPV = Elem<DT>::per_vec;
-  const float neg_m = -a.m, neg_mr = -a.mr;
+  const float neg_m = -a.m;
+  if (REF) {
+    const uint4 other[1] = {xr};
+    const float mr = fmaxf(a.mr, vecs_max<DT, 1>(other));
+    a.sr *= ex2(a.mr - mr);
+    a.mr = mr;
+  }
+  const float neg_mr = -a.mr;
   float s[2] = {0.f, 0.f}, u[2] = {0.f, 0.f}, w[2] = {0.f, 0.f}, sr[2] = {0.f, 0.f};
 #pragma unroll
   for (int g = 0; g < EPV / 4; ++g) {
@@ -60,35 +67,34 @@ __device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const 
   }
 }
 
-// The same where the references follow the largest logits seen.
+// The sums about a reference that is at least `top`.
+__device__ __forceinline__ void loss_raise(LossSums& a, float top) {
+  const float m = fmaxf(a.m, top), d = a.m - m, f = ex2(d);
+  a.u = (a.u + d * a.s) * f;
+  a.s *= f;
+  a.w *= f;
+  a.m = m;
+}
 template <int DT, bool REF>
 __device__ __forceinline__ void loss_push(LossSums& a, const uint4& x, const uint4& xr, float c) {
   const uint4 one[1] = {x};
-  const float m = fmaxf(a.m, vecs_max<DT, 1>(one)), d = a.m - m, f = ex2(d);
-  a.u = (a.u + d * a.s) * f;
-  a.s *= f;
-  a.m = m;
-  if (REF) {
-    a.w *= f;
-    const uint4 other[1] = {xr};
-    const float mr = fmaxf(a.mr, vecs_max<DT, 1>(other));
-    a.sr *= ex2(a.mr - mr);
-    a.mr = mr;
-  }
+  loss_raise(a, vecs_max<DT, 1>(one));
   loss_push_at<DT, REF>(a, x, xr, c);
 }
 
-// One wavefront folds its lanes' sums; uniform results.
+// One wavefront folds its lanes' sums; uniform results, about references whose lowest bit is set (it is the flag of the hand-off words).
 template <bool REF> __device__ __forceinline__ LossSums loss_fold_wave(const LossSums& a) {
   LossSums r = a;
-  r.m = wave_max_f(a.m);
-  const float d = r.m > kNegHuge ? a.m - r.m : 0.f, f = ex2(d);     // (nothing finite seen: the sums are 0, or a NaN)
+  const float top = wave_max_f(a.m);
+  r.m = __uint_as_float(__float_as_uint(top) | 1u);
+  const float d = top > kNegHuge ? a.m - r.m : 0.f, f = ex2(d);     // (nothing finite seen: the sums are 0, or a NaN)
   r.s = wave_sum_f(a.s * f);
   r.u = wave_sum_f((a.u + d * a.s) * f);
   if (REF) {
     r.w = wave_sum_f(a.w * f);
-    r.mr = wave_max_f(a.mr);
-    r.sr = wave_sum_f(a.sr * ex2(r.mr > kNegHuge ? a.mr - r.mr : 0.f));
+    const float topr = wave_max_f(a.mr);
+    r.mr = __uint_as_float(__float_as_uint(topr) | 1u);
+    r.sr = wave_sum_f(a.sr * ex2(topr > kNegHuge ? a.mr - r.mr : 0.f));
   }
   return r;
 }
@@ -99,7 +105,7 @@ template <bool REF> __device__ __forceinline__ LossSums loss_fold_wave(const Los
 struct LossRow {
   double lse, lse_ref;     // log-normalisers
   double H, kl;
-  float inv_s;             // 1 / s
+  double inv_s;            // 1 / s
   bool bad;
 };
 constexpr double kNat = 1.0 / (double)kLog2e;
@@ -107,11 +113,12 @@ constexpr double kTemperature = (double)kLog2e * kLn2 - 1.0;
 template <bool REF> __device__ __forceinline__ LossRow finish_loss_row(const LossSums& t, float c) {
   LossRow r;
   const bool ok = t.s > 0.f && t.s < INFINITY && fabsf(t.u) < INFINITY && t.m > kNegHuge && t.m < INFINITY;
-  const double s = ok ? (double)t.s : (double)NAN, l2 = log2_fine((float)s);
-  r.H = fmax(kNat * (l2 - (double)t.u / s), 0.0);
+  const float s = ok ? t.s : NAN;
+  const double l2 = log2_fine(s), inv = 1.0 / (double)s;
+  r.H = fmax(kNat * (l2 - (double)t.u * inv), 0.0);
   r.H = ok ? r.H : (double)NAN;
   r.lse = kNat * ((double)t.m + l2) + kTemperature * r.H;
-  r.inv_s = (float)(1.0 / s);
+  r.inv_s = inv;
   r.bad = !ok;
   r.lse_ref = 0.0;
   r.kl = 0.0;
@@ -120,7 +127,7 @@ template <bool REF> __device__ __forceinline__ LossRow finish_loss_row(const Los
     const double l2r = log2_fine(okr ? t.sr : NAN);
     r.lse_ref = kNat * ((double)t.mr + l2r);
     // (c next to the normalisers' difference: both large where the rows carry different offsets)
-    r.kl = fmax(kNat * ((double)t.w / s + ((double)c - (((double)t.m - (double)t.mr) + (l2 - l2r)))), 0.0);
+    r.kl = fmax(kNat * ((double)t.w * inv + ((double)c - (((double)t.m - (double)t.mr) + (l2 - l2r)))), 0.0);
     if (!ok || !okr || t.w != t.w) r.kl = (double)NAN;
     r.bad = r.bad || !okr;
   }
