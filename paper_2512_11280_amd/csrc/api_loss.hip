@@ -6,14 +6,23 @@
 namespace adasd {
 
 namespace {
-constexpr size_t kPerPosition = sizeof(LossCoef) + 2 * sizeof(double) + sizeof(float);
-constexpr size_t kLossFixed = (size_t)kMaxLossSlices * kXchgWords * sizeof(uint64_t) + (kTicketLossLen + 1 + kAddsUp) * sizeof(int32_t) + 7 * 256;
+constexpr size_t kSliceBytes = (kXchgWords + kResultWords) * sizeof(uint64_t);
+constexpr size_t kPerPosition = sizeof(LossCoef) + 2 * sizeof(double) + sizeof(float) + 2 * sizeof(int32_t) + kSlicesPerPosition * kSliceBytes;
+constexpr size_t kLossFixed = (size_t)kMaxLossSlices * kSliceBytes + (kTicketLossLen + 32 + kAddsUp) * sizeof(int32_t) +
+                              (kAddsUp + kAddsUp / 2) * sizeof(double) + 9 * 256;
 }  // namespace
 
-size_t loss_workspace_bytes_for(size_t positions) { return kLossFixed + (positions + 1) * kPerPosition; }
+// Room for the positions' arrays, and for the hand-off words of their slices at their longest (k_loss_join with a reference: 2048 vectors a
+// slice; longer rows than 64 of them have none).
+size_t loss_workspace_bytes_for(int64_t positions, int V, int dt) {
+  const int epv = dt == ADASD_BF16 ? 8 : 4;
+  const int64_t nv = ((int64_t)V + epv - 1) / epv, S = (nv + 8 * kBlock - 1) / (8 * kBlock);
+  const int64_t slices = S > 1 && S <= kMaxSplit ? S * positions - kMaxLossSlices : 0, more = (slices + kSlicesPerPosition - 1) / kSlicesPerPosition;
+  return kLossFixed + (size_t)((more > positions ? more : positions) + 1) * kPerPosition;
+}
 
-// (Offsets depend on the size of the workspace alone, and those of the words and counters not even on that: a call of another shape finds
-// them where the one before left them, at zero.)
+// (Offsets depend on the size of the workspace alone: a call of another shape finds words and counters where the one before left them, at
+// zero.)
 size_t loss_workspace_layout(size_t ws_bytes, LossWorkspace* ws, void* base) {
   if (ws_bytes <= kLossFixed) return 0;
   const size_t cap = (ws_bytes - kLossFixed) / kPerPosition;
@@ -23,9 +32,12 @@ size_t loss_workspace_layout(size_t ws_bytes, LossWorkspace* ws, void* base) {
     p += (bytes + 255) / 256 * 256;
     return at;
   };
-  ws->xchg = reinterpret_cast<uint64_t*>(take((size_t)kMaxLossSlices * kXchgWords * sizeof(uint64_t)));
+  ws->slices = kMaxLossSlices + (int64_t)cap * kSlicesPerPosition;
   ws->ticket = reinterpret_cast<int32_t*>(take(kTicketLossLen * sizeof(int32_t)));
-  ws->done = reinterpret_cast<int32_t*>(take((1 + kAddsUp) * sizeof(int32_t)));
+  ws->sets = reinterpret_cast<int32_t*>(take(2 * cap * sizeof(int32_t)));
+  ws->done = reinterpret_cast<int32_t*>(take((32 + kAddsUp) * sizeof(int32_t)));
+  ws->fresh = reinterpret_cast<double*>(take((kAddsUp + kAddsUp / 2) * sizeof(double)));
+  ws->xchg = reinterpret_cast<uint64_t*>(take((size_t)ws->slices * kSliceBytes));
   ws->coef = reinterpret_cast<LossCoef*>(take(cap * sizeof(LossCoef)));
   ws->term = reinterpret_cast<double*>(take(cap * sizeof(double)));
   ws->pair = reinterpret_cast<double*>(take(cap * sizeof(double)));
@@ -118,7 +130,7 @@ int adasd_loss_workspace_bytes(int B, int T, int V, adasd_dtype dt, size_t* byte
   if (!bytes) return ADASD_ERR_INVALID_ARG;
   const int rc = check_loss_shape(B, T, V, (int)dt);
   if (rc) return rc;
-  *bytes = loss_workspace_bytes_for((size_t)B * (size_t)T);
+  *bytes = loss_workspace_bytes_for((int64_t)B * T, V, (int)dt);
   return ADASD_OK;
 }
 
@@ -142,7 +154,7 @@ int adasd_token_logprob(const adasd_rows* a, void* stream) { return token_logpro
 int adasd_test_logprob_unarrived(const adasd_rows* a, void* stream) { return token_logprob(a, stream, kNotThere); }
 int adasd_test_logprob_given_up(const adasd_rows* a, void* stream) { return token_logprob(a, stream, kGivesUp); }
 
-int adasd_token_logprob_grad(const adasd_rows* a, const float* dlogprob, const float* dentropy, void* stream) {
+static int token_logprob_grad(const adasd_rows* a, const float* dlogprob, const float* dentropy, void* stream, WordWait wait) {
   LossRows rows;
   LossWorkspace ws{};
   const int rc = loss_setup(a, nullptr, 0, 0, false, &rows, &ws);
@@ -151,11 +163,23 @@ int adasd_token_logprob_grad(const adasd_rows* a, const float* dlogprob, const f
   if (!dlogprob || !a->dlogits) return ADASD_ERR_INVALID_ARG;
   if (!aligned_to(dlogprob, 4) || !aligned_to(dentropy, 4)) return ADASD_ERR_MISALIGNED;
   LossTerm f{};
-  f.wait = kWaits;
+  f.wait = wait;
   f.kind = kLogprob;
   f.dlogprob = dlogprob;
   f.dentropy = dentropy;
   return run(rows, (int)a->dt, f, ws, stream);
+}
+
+int adasd_token_logprob_grad(const adasd_rows* a, const float* dlogprob, const float* dentropy, void* stream) {
+  return token_logprob_grad(a, dlogprob, dentropy, stream, kWaits);
+}
+
+// For the tests, as above: the slices form the others' sums from the logits whatever has been sent, or do not wait for them.
+int adasd_test_logprob_grad_unarrived(const adasd_rows* a, const float* dlogprob, const float* dentropy, void* stream) {
+  return token_logprob_grad(a, dlogprob, dentropy, stream, kNotThere);
+}
+int adasd_test_logprob_grad_given_up(const adasd_rows* a, const float* dlogprob, const float* dentropy, void* stream) {
+  return token_logprob_grad(a, dlogprob, dentropy, stream, kGivesUp);
 }
 
 int adasd_policy_loss(const adasd_rows* a, const adasd_policy_args* p, void* stream) {

@@ -218,20 +218,26 @@ struct LossCoef {       // of a position: its gradient row is a 1[j = x] + 2^(x_
   float m, a, k0, k1, k2, c, pad[2];
 };
 struct LossWorkspace {
-  uint64_t* xchg;       // [kMaxLossSlices][kXchgWords] hand-off words of the slices, zero between launches
-  int32_t* ticket;      // [kTicketLossLen] arrival words of the rows cut into slices, zero between launches
-  int32_t* done;        // [1 + kAddsUp] positions (or pairs) that are done, and positions of each pair; zero between launches
-  LossCoef* coef;       // [n]
-  double* term;         // [n] what a position adds to the loss or to its sequence's score
-  double* pair;         // [n] what a pair adds to the loss
-  float* seq;           // [n] derivative of the loss by a sequence's score
+  int32_t* ticket;      // [kTicketLossLen] arrival words of the rows that k_loss_sums cuts into slices (see Arrivals), zero between launches
+  int32_t* sets;        // [positions][2] the same of k_loss_join
+  int32_t* done;        // [32 + kAddsUp] positions (or pairs) that are done, and positions of each pair; zero between launches
+  double* fresh;        // [kAddsUp + kAddsUp / 2] terms of positions, and of pairs, that the last one done adds up; zero between launches
+  uint64_t* xchg;       // [slices][kXchgWords + kResultWords] hand-off words, zero between launches
+  LossCoef* coef;       // [positions]
+  double* term;         // [positions] what a position adds to the loss or to its sequence's score (of more than kAddsUp)
+  double* pair;         // [positions] what a pair adds to the loss
+  float* seq;           // [positions] derivative of the loss by a sequence's score
+  int64_t slices;
 };
+constexpr int kResultWords = 4;                          // 64-bit words of the numbers of a gradient row, sent to a slice
 constexpr int kMaxLossSlices = 8 * kResidentGroups;      // of all rows that are cut into more than one (scan_split)
+constexpr int kSlicesPerPosition = 4;                    // hand-off words of so many more come with each position of a workspace
 constexpr int kTicketLossLen = 32768;
 // Up to so many positions the last one done adds up the loss, which saves a launch or two (3 to 5 us); of more, that many additions to one
 // counter come one after the other, and a launch of its own is lost beside what they take.
-constexpr int kAddsUp = 4096;
-size_t loss_workspace_bytes_for(size_t positions);
+constexpr int kAddsUp = 4096, kJoinAddsUp = 256;
+constexpr int kJoinResident = 4 * 256;                   // workgroups of k_loss_join that the chip holds
+size_t loss_workspace_bytes_for(int64_t positions, int V, int dt);
 size_t loss_workspace_layout(size_t ws_bytes, LossWorkspace* ws, void* base);
 hipError_t launch_loss(const LossRows& rows, int dt, LossTerm term, const LossWorkspace& ws, hipStream_t st);
 

@@ -2,12 +2,14 @@
 //
 // A gradient row needs the row's normaliser (and entropy, and KL) before its first element, and the preference loss those of whole
 // sequences.
-//   k_loss_sums  (slices of rows) the sums of each slice (loss_device.h).  One workgroup of a row folds them (hand_off), settles the
-//                position: what is reported of it, and the five numbers of its gradient row.  The position that is done last adds up
-//                the loss; of a pair's sequences, settles the pair.
-//   k_loss_grad  (slices of rows) reads the logits again and forms the gradient.
-//   k_loss_fused (a workgroup per row, which stays in registers) both in one, where the gradient needs nothing but its own row.
-//   k_loss_pairs, k_loss_total: pairs and the sum of the loss where there are many positions.
+//   k_loss_join  gradients that need nothing but their own row: the row stays in the registers of its workgroups between the sums and
+//                the gradient, so that everything is read once and written once.  Rows of up to 2048 vectors: one to four wavefronts
+//                each; longer ones: slices, whose workgroups exchange their sums.
+//   k_loss_sums  (slices of rows) the sums alone: log-probabilities, the preference loss, rows too long for k_loss_join.  One workgroup of
+//                a row folds its slices (hand_off).
+//   k_loss_grad  (pieces of rows) reads the logits again and forms the gradient.
+// Either way one wavefront settles the position: what is reported of it, and the five numbers of its gradient row.  Of few positions
+// the one done last adds up the loss, or settles its pair; of many k_loss_pairs and k_loss_total do.
 // Sums over positions and sequences are in 64 bits and in a fixed order, whoever forms them.
 #include "loss_device.h"
 #include "sample_device.h"
@@ -18,12 +20,6 @@ namespace {
 
 using namespace sampling;
 
-// Vectors v0 .. v1 of a row that slice s of S works on.
-__device__ __forceinline__ void slice_of(int nv, int s, int S, int& v0, int& v1) {
-  const int chunk = slice_vectors(nv, S);
-  v0 = min(s * chunk, nv);
-  v1 = min(v0 + chunk, nv);
-}
 template <int DT> __device__ __forceinline__ uint4 load_vec_of(const char* row, int idx, int V) {
   return idx < V / Elem<DT>::per_vec ? load_vec_any(row, idx) : load_last_vec<DT>(row, V);
 }
@@ -58,11 +54,12 @@ template <int DT> __device__ __forceinline__ void ask_logit(PositionIn& in, cons
   in.z = load_elem<DT>(row, in.x >= 0 && in.x < V ? in.x : 0);
 }
 
-// What is reported of a position (lane 0 writes it), and the numbers of its gradient row, by one wavefront from the sums of the whole row.
+// What is reported of a position, and the numbers of its gradient row, from the sums of the whole row.  Two neighbouring lanes (or more
+// pairs of them) go through it together; the one that `writes` reports.
 template <bool REF>
 __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const LossTerm& f, int r, const PositionIn& in, const LossSums& sums,
-                                                    float c, double& term) {
-  const int lane = threadIdx.x & 63;
+                                                    float c, bool writes, double& term) {
+  const bool odd = threadIdx.x & 1;
   const bool known = in.x >= 0 && in.x < rows.V;
   const LossRow row = finish_loss_row<REF>(sums, c);
   const double lp = known ? (double)in.z - row.lse : (double)NAN;
@@ -74,8 +71,9 @@ __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const 
     by_entropy = (double)in.h;
   } else if (f.kind == kPolicy) {
     // one exponential for both ratios: the old policy's in the even lanes, the reference's in the odd ones
-    const double grown = expm1_fine(lane & 1 ? (double)in.ref - lp : lp - (double)in.old);
-    const double A = (double)in.a, ratio = f.old_logprob ? 1.0 + __shfl(grown, 0) : lp == lp ? 1.0 : lp, grown_ref = __shfl(grown, 1);
+    const double mine = expm1_fine(odd ? (double)in.ref - lp : lp - (double)in.old), other = __shfl_xor(mine, 1);
+    const double grown_ref = odd ? mine : other, grown = odd ? other : mine;
+    const double A = (double)in.a, ratio = f.old_logprob ? 1.0 + grown : lp == lp ? 1.0 : lp;
     if (A != 0.0) {
       const double free = ratio * A, held = fmin(fmax(ratio, 1.0 - (double)f.clip_low), 1.0 + (double)f.clip_high) * A;
       const bool clipped = held < free;
@@ -97,7 +95,7 @@ __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const 
     term = w * (lp - (f.ref_logprob ? (double)in.ref : 0.0));
     a = w;
   }
-  if (lane == 0) {
+  if (writes) {
     if (rows.logprob) rows.logprob[r] = (float)lp;
     if (rows.entropy) rows.entropy[r] = (float)row.H;
     if (rows.status) rows.status[r] = (known ? 0u : (uint32_t)ADASD_ST_BAD_TOKEN) | (row.bad ? (uint32_t)ADASD_ST_NONFINITE : 0u);
@@ -131,20 +129,33 @@ __device__ __forceinline__ void report_nothing(const LossRows& rows, const LossT
   if (f.kl) f.kl[r] = 0.f;
 }
 
-// ---- sums over positions.  One wavefront; the order of the additions is the same whether other workgroups' terms are read in the launch
-// that forms them (FRESH) or in a later one.
-template <bool FRESH> __device__ __forceinline__ double wave_total(const double* v, int n) {
+// ---- sums over positions, by one wavefront.  Where the terms come from other workgroups of the same launch (FRESH) they are 64-bit words that
+// say themselves that they are there (the lowest bit of the fraction is set; a cleared word is 0), and are cleared as they are read.  The
+// order of the additions is the same either way.
+__device__ __forceinline__ double flagged_term(double v) { return __longlong_as_double(__double_as_longlong(v) | 1ll); }
+template <bool FRESH> __device__ __forceinline__ double wave_total(double* v, int n) {
   const int lane = threadIdx.x & 63;
   double t = 0.0;
   for (int base = 0; base < n; base += 8 * 64) {
     double x[8];
+    auto look = [&] {
+      bool there = true;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = base + k * 64 + lane;
+        x[k] = i < n ? (FRESH ? ld_agent(v + i) : v[i]) : 0.0;
+        there = there && (i >= n || (__double_as_longlong(x[k]) & 1));
+      }
+      return __all(there) != 0;
+    };
+    bool there = look() || !FRESH;
+    // (all had been sent when the last one was counted: this ends at once, unless calls that share a workspace have not been ordered)
+    for (int polls = kWaitPolls; !there && polls > 0; --polls) there = look();
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const int i = base + k * 64 + lane;
-      x[k] = i < n ? (FRESH ? ld_agent(v + i) : v[i]) : 0.0;
+      t += there ? x[k] : (double)NAN;
+      if (FRESH && base + k * 64 + lane < n) st_agent(v + base + k * 64 + lane, 0.0);
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) t += x[k];
   }
   return wave_sum(t);
 }
@@ -154,7 +165,8 @@ __device__ __forceinline__ double softplus(double v) { return fmax(v, 0.0) + log
 // A pair's loss and slope from the terms of its positions, by one wavefront (lane 0 writes).
 template <bool FRESH> __device__ __forceinline__ void settle_pair(const LossTerm& f, const LossWorkspace& ws, int i, int T) {
   const int P = f.P;
-  const double chosen = wave_total<FRESH>(ws.term + (size_t)i * T, T), rejected = wave_total<FRESH>(ws.term + (size_t)(P + i) * T, T);
+  double* terms = FRESH ? ws.fresh : ws.term;
+  const double chosen = wave_total<FRESH>(terms + (size_t)i * T, T), rejected = wave_total<FRESH>(terms + (size_t)(P + i) * T, T);
   const double beta = (double)f.beta, e = (double)f.smoothing, D = chosen - rejected;
   double m, loss, slope;
   if (f.pair_kind == 1) {
@@ -177,7 +189,9 @@ template <bool FRESH> __device__ __forceinline__ void settle_pair(const LossTerm
   const double w = f.pair_weight ? (double)f.pair_weight[i] : 1.0 / (double)P;
   const double scale = w * (f.grad_scale ? (double)*f.grad_scale : 1.0);
   if ((threadIdx.x & 63) != 0) return;
-  st_agent(ws.pair + i, w != 0.0 ? w * loss : 0.0);
+  const double part = w != 0.0 ? w * loss : 0.0;
+  if (FRESH) st_agent(ws.fresh + kAddsUp + i, flagged_term(part));
+  else ws.pair[i] = part;
   ws.seq[i] = w != 0.0 ? (float)(scale * slope) : 0.f;
   ws.seq[P + i] = w != 0.0 ? (float)(-scale * slope) : 0.f;
   if (f.pair_loss) f.pair_loss[i] = (float)loss;
@@ -188,9 +202,8 @@ template <bool FRESH> __device__ __forceinline__ void settle_pair(const LossTerm
   }
 }
 
-// Whether this is the last of n to come to a counter, which is zero again then: all that the others stored before is to be read.
+// Whether this is the last of n to come to a counter, which is zero again then.
 __device__ __forceinline__ bool last_of(int32_t* counter, int n) {
-  stores_before_loads();
   if (!last_to_add(add_arrival(counter), n)) return false;
   set_arrival(counter, 0);
   return true;
@@ -198,30 +211,35 @@ __device__ __forceinline__ bool last_of(int32_t* counter, int n) {
 // Position r is settled (one wavefront): the last of a pair settles the pair, the last of all adds up the loss.
 __device__ __forceinline__ void position_done(const LossRows& rows, const LossTerm& f, const LossWorkspace& ws, int r, double term) {
   if (!f.loss) return;
-  if ((threadIdx.x & 63) == 0) st_agent(ws.term + r, term);
-  if (!f.adds_up) return;
+  const bool first = (threadIdx.x & 63) == 0;
+  if (!f.adds_up) {
+    if (first) ws.term[r] = term;
+    return;
+  }
+  if (first) st_agent(ws.fresh + r, flagged_term(term));
   int n = rows.n;
-  const double* v = ws.term;
+  double* v = ws.fresh;
   if (f.kind == kPreference) {
     const int b = r / rows.T, i = b < f.P ? b : b - f.P;
-    if (!last_of(ws.done + 1 + i * ticket_stride(f.P, kAddsUp), 2 * rows.T)) return;
+    if (!last_of(ws.done + 32 + i * ticket_stride(f.P, kAddsUp), 2 * rows.T)) return;
     settle_pair<true>(f, ws, i, rows.T);
     n = f.P;
-    v = ws.pair;
+    v += kAddsUp;
   }
   if (!last_of(ws.done, n)) return;
   const double t = wave_total<true>(v, n);
-  if ((threadIdx.x & 63) == 0) *f.loss = (float)t;
+  if (first) *f.loss = (float)t;
 }
 
-// Sums of a whole row by one wavefront (where the slices' records did not arrive, which never happens to calls that are ordered as they
-// have to be).
-template <int DT, bool REF> __device__ __noinline__ LossSums wave_row_sums(const char* row, const char* ref, int V, float c) {
+// Sums of the vectors v0 .. v1 of a row by one wavefront (where the slices' records did not arrive, which never happens to calls that are
+// ordered as they have to be).
+template <int DT, bool REF> __device__ __noinline__ LossSums wave_sums(const char* row, const char* ref, int V, int v0, int v1, float c) {
   LossSums a = loss_empty();
 #pragma unroll 1
-  for (int idx = threadIdx.x & 63; idx < vectors_of<DT>(V); idx += 64) {
-    const uint4 x = load_vec_of<DT>(row, idx, V);
-    loss_push<DT, REF>(a, x, REF ? load_vec_of<DT>(ref, idx, V) : x, c);
+  for (int idx = v0 + (threadIdx.x & 63); idx < v1; idx += 64) {
+    const uint4 x[1] = {load_vec_of<DT>(row, idx, V)}, xr[1] = {REF ? load_vec_of<DT>(ref, idx, V) : x[0]};
+    loss_raise<DT, REF, 1>(a, x, xr);
+    loss_push_at<DT, REF>(a, x[0], xr[0], c);
   }
   return loss_fold_wave<REF>(a);
 }
@@ -261,7 +279,7 @@ template <int DT, bool REF> __global__ void __launch_bounds__(kBlock) k_loss_sum
 #pragma unroll
     for (int k = 0; k < kSumsBatch; ++k) {
       x[k] = next[k];
-      if (REF) xr[k] = nextr[k];
+      xr[k] = REF ? nextr[k] : next[k];
     }
     if (base + kSumsBatch * kBlock < v1) {
 #pragma unroll
@@ -271,7 +289,7 @@ template <int DT, bool REF> __global__ void __launch_bounds__(kBlock) k_loss_sum
         if (REF) nextr[k] = load(ref, idx);
       }
     }
-    loss_raise(a, vecs_max<DT, kSumsBatch>(x));
+    loss_raise<DT, REF, kSumsBatch>(a, x, xr);
 #pragma unroll
     for (int k = 0; k < kSumsBatch; ++k)
       if (base + k * kBlock < v1) loss_push_at<DT, REF>(a, x[k], REF ? xr[k] : x[k], c);
@@ -293,17 +311,17 @@ template <int DT, bool REF> __global__ void __launch_bounds__(kBlock) k_loss_sum
       a = LossSums{p.mp, p.sp, p.up, p.uq, p.mq, p.sq};
     }
     a = loss_fold_wave<REF>(a);
-    if (__builtin_expect(!arrived, 0)) a = wave_row_sums<DT, REF>(row, ref, V, c);
+    if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, nv, c);
   }
   double term;
-  const LossCoef k = settle_position<REF>(rows, f, r, in, a, c, term);
+  const LossCoef k = settle_position<REF>(rows, f, r, in, a, c, lane == 0, term);
   if (lane == 0) ws.coef[r] = k;
   position_done(rows, f, ws, r, term);
 }
 
 __global__ void __launch_bounds__(64) k_loss_pairs(LossTerm f, int T, LossWorkspace ws) { settle_pair<false>(f, ws, blockIdx.x, T); }
 
-__global__ void __launch_bounds__(64) k_loss_total(const double* v, int n, float* out) {
+__global__ void __launch_bounds__(64) k_loss_total(double* v, int n, float* out) {
   const double t = wave_total<false>(v, n);
   if (threadIdx.x == 0) *out = (float)t;
 }
@@ -368,136 +386,304 @@ __device__ __forceinline__ void grad_vec(const uint4& x, const uint4& xr, const 
   }
 }
 
-template <int DT, bool ENT, bool REF>
-__global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int S, LossWorkspace ws, int by_sequence) {
+// Whether the gradient row is zeros, whatever the logits are.
+__device__ __forceinline__ bool zero_row(const LossCoef& k) { return k.a == 0.f && k.k0 == 0.f && k.k1 == 0.f && k.k2 == 0.f; }
+template <int DT> __device__ __forceinline__ void zero_vec(char* row, int idx, int V) {
+  const float g[Elem<DT>::per_vec] = {};
+  store_grad<DT>(row, idx, V, g);
+}
+template <int DT, bool REF>
+__device__ __forceinline__ void emit_vec(char* out, int idx, int V, int x, const uint4& z, const uint4& zr, const LossCoef& k, bool ent) {
   constexpr int EPV = Elem<DT>::per_vec;
-  const int r = blockIdx.x, b = r / rows.T, t = r - b * rows.T, V = rows.V;
-  LossCoef k = scalar_load(ws.coef + r);
-  if (by_sequence) {
-    const float d = scalar_load(ws.seq + b);
-    k.a *= d;
-    k.k0 = d == 0.f ? 0.f : k.k0 * d;
-    if (d == 0.f) k.a = 0.f;
-  }
-  char* out = const_cast<char*>(row_at<DT>(rows.g, b, t));
-  const char* row = row_at<DT>(rows.z, b, t);
-  const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
-  int v0, v1;
-  slice_of(vectors_of<DT>(V), blockIdx.y, S, v0, v1);
   float g[EPV];
-  if (k.a == 0.f && k.k0 == 0.f && k.k1 == 0.f && k.k2 == 0.f) {
+  if (ent) grad_vec<DT, true, REF>(z, zr, k, g);
+  else grad_vec<DT, false, REF>(z, zr, k, g);
+  if (idx == x / EPV) {
 #pragma unroll
-    for (int i = 0; i < EPV; ++i) g[i] = 0.f;
-    for (int idx = v0 + threadIdx.x; idx < v1; idx += kBlock) store_grad<DT>(out, idx, V, g);
-    return;
+    for (int i = 0; i < EPV; ++i) g[i] += idx * EPV + i == x ? k.a : 0.f;
   }
-  const int x = rows.tokens[r];
-  for (int idx = v0 + threadIdx.x; idx < v1; idx += kBlock) {
-    const uint4 v = load_vec_of<DT>(row, idx, V);
-    grad_vec<DT, ENT, REF>(v, REF ? load_vec_of<DT>(ref, idx, V) : v, k, g);
-    if (idx == x / EPV) {
-#pragma unroll
-      for (int i = 0; i < EPV; ++i) g[i] += idx * EPV + i == x ? k.a : 0.f;
+  store_grad<DT>(out, idx, V, g);
+}
+
+// Pieces of rows of `per` vectors, a wavefront each.
+constexpr int kPiece = 8 * 64, kMostPieces = 2048;      // (2^20 rows: no more than 2^31 pieces)
+constexpr uint32_t kMostGroups = 1u << 22;
+template <int DT, bool REF>
+__global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces, int per, LossWorkspace ws, int by_sequence, int ent) {
+  const int lane = threadIdx.x & 63, V = rows.V, nv = vectors_of<DT>(V);
+  const uint32_t step = gridDim.x * kWaves, units = (uint32_t)rows.n * (uint32_t)pieces;
+  for (uint32_t unit = blockIdx.x * kWaves + uniform(threadIdx.x >> 6); unit < units; unit += step) {
+    const int r = (int)(unit / (uint32_t)pieces), piece = (int)(unit - (uint32_t)r * (uint32_t)pieces), b = r / rows.T, t = r - b * rows.T;
+    LossCoef k = scalar_load(ws.coef + r);
+    if (by_sequence) {
+      const float d = scalar_load(ws.seq + b);
+      k.a = d == 0.f ? 0.f : k.a * d;
+      k.k0 = d == 0.f ? 0.f : k.k0 * d;
     }
-    store_grad<DT>(out, idx, V, g);
+    char* out = const_cast<char*>(row_at<DT>(rows.g, b, t));
+    const char* row = row_at<DT>(rows.z, b, t);
+    const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
+    const int v0 = piece * per, v1 = min(v0 + per, nv);
+    if (zero_row(k)) {
+      for (int idx = v0 + lane; idx < v1; idx += 64) zero_vec<DT>(out, idx, V);
+      continue;
+    }
+    const int x = rows.tokens[r];
+    for (int idx = v0 + lane; idx < v1; idx += 64) {
+      const uint4 z = load_vec_of<DT>(row, idx, V);
+      emit_vec<DT, REF>(out, idx, V, x, z, REF ? load_vec_of<DT>(ref, idx, V) : z, k, ent);
+    }
   }
 }
 
-// ---- Many rows: one workgroup of T threads per row.  The row's first NB vectors per thread stay in registers (raw) from the load to
-// the gradient, so that they are read once; what is longer, and the reference's row, is read again (from the cache behind the L2s,
-// where the few hundred rows in work fit).
-template <int W> struct FusedLoss {
+// ---- Everything in one launch, where a gradient row needs nothing but its own row.  A workgroup of four wavefronts has 4 / WPR rows, or
+// (WPR = 4, S > 1) a slice of one.  The raw vectors, up to NB per thread and row, stay in its registers from the load to the gradient.
+//
+// The slices hand their sums to one workgroup (hand_off); it settles the position and sends the numbers of the gradient row to each of the
+// others, into words that this slice alone reads and clears.  (All slices reading all records: 16 x 128256 in 63 slices waited 7.4 us for
+// them; a count of those that have read one result, kept to clear it: 4.5 us more.)  Slices of a row are consecutive workgroups, and
+// workgroups are started in order on each die, so who is waited for has mostly started; but other streams' work may hold the chip, and two calls
+// that wait on two streams could hold each other's places.  So every wait is bounded: a slice that has waited in vain leaves a mark in
+// the place of its result and ends, and who comes to send the result finds the mark and does the slice's part as well, from the logits
+// (which are whole there: only the slice itself would have put its gradient in their place).
+template <int W> struct JoinShared {
   LossSums sums[W];
-  LossCoef coef;
+  float c[kWaves];
+  LossCoef coef[kWaves];
+  int role;             // of a slice
+  uint64_t left;        // slices whose part is to be done as well
 };
-constexpr int kRefAhead = 4;      // vectors of the reference's row on their way
-template <int DT, bool ENT, bool REF, int T, int NB>
-__global__ void __launch_bounds__(T, 4) k_loss_fused(LossRows rows, LossTerm f, LossWorkspace ws) {
-  constexpr int EPV = Elem<DT>::per_vec, W = T / 64;
-  __shared__ FusedLoss<W> sh;
-  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = rows.V, whole = V / EPV, nv = vectors_of<DT>(V);
-  const int b = r / rows.T, t = r - b * rows.T;
-  char* out = const_cast<char*>(row_at<DT>(rows.g, b, t));
-  float g[EPV];
-  auto zeros = [&] {
-#pragma unroll
-    for (int i = 0; i < EPV; ++i) g[i] = 0.f;
-    for (int idx = tid; idx < nv; idx += T) store_grad<DT>(out, idx, V, g);
+enum { kWaitsFor = 0, kSettles = 1, kLeaves = 2 };
+constexpr uint64_t kLeft = 2;        // in a result's first word: its slice has ended without it
+// The slice's result, waited for and cleared (one wavefront).  False: the mark is left.
+__device__ __forceinline__ bool await_result(uint64_t* at, WordWait wait, LossCoef& k) {
+  const int lane = threadIdx.x & 63;
+  uint64_t w = 1;
+  auto look = [&](int polls) {
+    for (;; --polls) {
+      if (lane < kResultWords) w = __hip_atomic_load(at + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (__all((w & 1ull) != 0)) return true;
+      if (polls <= 0) return false;
+      __builtin_amdgcn_s_sleep(1);
+    }
   };
-  if (!position_counts(rows, r)) {
-    if (tid == 0) report_nothing(rows, f, r);
-    zeros();
-    if (wave == 0) position_done(rows, f, ws, r, 0.0);
-    return;
+  if (!look(wait == kWaits ? kWaitPolls : 0)) {
+    uint64_t seen = 0;
+    if (exchange_arrival(at, seen, kLeft)) return false;
+    if (!look(kWaitPolls)) return false;          // (the result's other words have been sent with its first)
   }
-  PositionIn in = ask_position(rows, f, r, b);
+  if (lane < kResultWords) __hip_atomic_store(at + lane, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  k.m = lane_value(word_lo(w), 0);
+  k.a = lane_value(word_hi(w), 0);
+  k.k0 = lane_value(word_hi(w), 1);
+  k.k1 = lane_value(word_hi(w), 2);
+  k.k2 = lane_value(word_hi(w), 3);
+  return true;
+}
+// The result to all slices but `own`, lane by lane.  Returns what stood in the first word (kLeft: the slice has ended).
+__device__ __forceinline__ uint64_t send_results(uint64_t* at, int S, int own, const LossCoef& k) {
+  const int lane = threadIdx.x & 63;
+  if (lane >= S || lane == own) return 0;
+  at += lane * kResultWords;
+  __hip_atomic_store(at + 1, record_word(1u, k.k0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(at + 2, record_word(1u, k.k1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(at + 3, record_word(1u, k.k2), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return __hip_atomic_exchange(at, record_word(bits_of(k.m), k.a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Wavefronts per SIMD that the registers are limited for (64 of data and about 50 more: four; 16: eight).
+constexpr int join_waves(int nb, bool ref) { return !ref ? (nb <= 4 ? 8 : nb <= 8 ? 6 : 4) : (nb <= 2 ? 7 : nb <= 4 ? 5 : 4); }
+template <int DT, bool REF, int NB, int WPR>
+__global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(NB, REF)) k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, LossWorkspace ws) {
+  constexpr int RPB = WPR < kWaves ? kWaves / WPR : 1, TR = 64 * WPR;          // rows per workgroup, threads per row
+  __shared__ JoinShared<WPR < kWaves ? kWaves : WPR> sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), V = rows.V, nv = vectors_of<DT>(V);
+  const int r0 = RPB > 1 ? blockIdx.x * RPB : blockIdx.x / S, s = RPB > 1 ? 0 : blockIdx.x - r0 * S;
+  const int sub = wave / WPR, r = r0 + sub, me = tid & (TR - 1);
+  const bool here = r < rows.n;
+  const int b = here ? r / rows.T : 0, t = here ? r - b * rows.T : 0;
+  const bool on = here && position_counts(rows, r);
   const char* row = row_at<DT>(rows.z, b, t);
   const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
-  auto load = [&](const char* from, int j) {
-    const int idx = tid + j * T;
-    if ((j + 1) * T <= whole) return load_vec_any(from, idx);
-    return idx < nv ? load_vec_of<DT>(from, idx, V) : neutral_vec<DT>();
-  };
-  uint4 v[NB], q[kRefAhead];
-#pragma unroll
-  for (int j = 0; j < NB; ++j) v[j] = load(row, j);
-  if (REF) {
-#pragma unroll
-    for (int j = 0; j < kRefAhead; ++j) q[j] = load(ref, j);
-  }
-  ask_logit<DT>(in, row, V);
-  const float c = REF ? ref_shift<DT>(row, ref, in.x, V) : 0.f;
-  LossSums a = loss_empty();
-  a.m = vecs_max<DT, NB>(v);
-#pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    if (j * T < nv) loss_push_at<DT, REF>(a, v[j], REF ? q[j % kRefAhead] : v[j], c);
-    if (REF && j + kRefAhead < NB) q[j % kRefAhead] = load(ref, j + kRefAhead);
-  }
-  for (int idx = tid + NB * T; idx < nv; idx += T) {
-    const uint4 x = load_vec_of<DT>(row, idx, V);
-    loss_push<DT, REF>(a, x, REF ? load_vec_of<DT>(ref, idx, V) : x, c);
-  }
-  a = loss_fold_wave<REF>(a);
-  if (lane == 0) sh.sums[wave] = a;
-  __syncthreads();
-  double term = 0.0;
+  const int v0 = min(s * chunk, nv), v1 = min(v0 + chunk, nv);
+  // what the positions are settled from, a pair of lanes for each row of the workgroup
+  const int i = RPB > 1 ? min(lane >> 1, RPB - 1) : 0, ri = min(r0 + i, rows.n - 1), bi = ri / rows.T;
+  PositionIn in{};
+  bool on_i = on;
   if (wave == 0) {
-    a = loss_fold_wave<REF>(lane < W ? sh.sums[lane] : loss_empty());
-    const LossCoef mine = settle_position<REF>(rows, f, r, in, a, c, term);
-    if (lane == 0) sh.coef = mine;
+    if (RPB > 1) on_i = r0 + i < rows.n && position_counts(rows, ri);
+    if (on_i && s == S - 1) in = ask_position(rows, f, ri, bi);
   }
-  if (REF) {
+  uint4 v[NB], q[NB];
+  int x = -1;
+  if (here) x = rows.tokens[r];
+  if (on) {
+    const int full = min(v1, V / Elem<DT>::per_vec);
+    auto load = [&](const char* from, int j) {
+      const int idx = v0 + me + j * TR;
+      if (v0 + (j + 1) * TR <= full) return load_vec_any(from, idx);
+      return idx < v1 ? load_vec_of<DT>(from, idx, V) : neutral_vec<DT>();
+    };
 #pragma unroll
-    for (int j = 0; j < kRefAhead; ++j) q[j] = load(ref, j);
+    for (int j = 0; j < NB; ++j) v[j] = load(row, j);
+    if (REF) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) q[j] = load(ref, j);
+    }
+  }
+  const char* row_i = row_at<DT>(rows.z, bi, ri - bi * rows.T);
+  if (wave == 0 && on_i && s == S - 1) ask_logit<DT>(in, row_i, V);
+  float c = 0.f;
+  if (on) {
+    if (REF) c = ref_shift<DT>(row, ref, x, V);
+    LossSums a = loss_empty();
+    loss_raise<DT, REF, NB>(a, v, REF ? q : v);
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      if (v0 + j * TR < v1) loss_push_at<DT, REF>(a, v[j], REF ? q[j] : v[j], c);
+    a = loss_fold_wave<REF>(a);
+    if (lane == 0) {
+      sh.sums[wave] = a;
+      sh.c[sub] = c;
+    }
   }
   __syncthreads();
-  const LossCoef k = sh.coef;
-  if (k.a == 0.f && k.k0 == 0.f && k.k1 == 0.f && k.k2 == 0.f) {
-    zeros();
-    if (wave == 0) position_done(rows, f, ws, r, term);
+  x = uniform(x);
+  double term = 0.0;
+  bool settles = S == 1;
+  uint64_t found = 0;
+  uint64_t* words = ws.xchg + (size_t)r * S * (kXchgWords + kResultWords);      // (S > 1: the records, then the results)
+  uint64_t* results = words + S * kXchgWords;
+  if (wave == 0) {
+    LossCoef k{};
+    int role = kWaitsFor;
+    if (RPB > 1 || on) {
+      LossSums a;
+      if (WPR > kWaves) {
+        a = loss_fold_wave<REF>(lane < WPR ? sh.sums[lane] : loss_empty());
+      } else {
+        a = sh.sums[i * WPR];
+#pragma unroll
+        for (int n = 1; n < WPR; ++n) a = loss_merge<REF>(a, sh.sums[i * WPR + n]);
+      }
+      if (RPB == 1 && S > 1) {
+        a = loss_flagged<REF>(a);
+        bool arrived = true;
+        uint64_t w[kXchgWords];
+        pack_pair(PairRecord{a.m, a.s, a.u, REF ? a.mr : a.m, REF ? a.sr : 0.f, REF ? a.w : 0.f}, w);
+        settles = hand_off(PlainWords{words}, s, S, Arrivals{ws.sets, 0, r, rows.n, true}, f.wait,
+                           [&] {
+                             if (s == S - 1) return;
+                             in = ask_position(rows, f, r, b);
+                             ask_logit<DT>(in, row, V);
+                           },
+                           w, arrived);
+        if (settles) {
+          a = loss_empty();
+          if (lane < S) {
+            const PairRecord p = unpack_pair(w);
+            a = LossSums{p.mp, p.sp, p.up, p.uq, p.mq, p.sq};
+          }
+          a = loss_fold_wave<REF>(a);
+          if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, nv, c);
+        } else if (!await_result(results + s * kResultWords, f.wait, k)) {
+          role = kLeaves;
+        }
+      }
+      if (settles) {
+        role = kSettles;
+        const bool writes = on_i && (RPB > 1 ? !(lane & 1) && lane < 2 * RPB : lane == 0);
+        const LossCoef settled = settle_position<REF>(rows, f, ri, in, a, REF ? sh.c[i] : 0.f, writes, term);
+        if (on_i) k = settled;
+        else term = 0.0;
+        if (RPB == 1 && S > 1) found = send_results(results, S, s, k);
+      }
+      if (RPB == 1) k.c = c;
+    }
+    if (RPB > 1 ? !(lane & 1) && lane < 2 * RPB && r0 + i < rows.n : lane == 0) {
+      sh.coef[i] = k;
+      sh.role = role;
+      if (!on_i && s == 0) report_nothing(rows, f, ri);
+      if (!rows.g.base) ws.coef[ri] = k;
+      if (RPB > 1 && f.loss) ws.term[ri] = term;
+    }
+  }
+  __syncthreads();
+  if (!here || (RPB == 1 && sh.role == kLeaves)) return;
+  char* out = rows.g.base ? const_cast<char*>(row_at<DT>(rows.g, b, t)) : nullptr;
+  const LossCoef k = sh.coef[sub];
+  if (out) {
+    if (zero_row(k)) {
+      for (int idx = v0 + me; idx < v1; idx += TR) zero_vec<DT>(out, idx, V);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const int idx = v0 + me + j * TR;
+        if (idx < v1) emit_vec<DT, REF>(out, idx, V, x, v[j], REF ? q[j] : v[j], k, ent);
+      }
+    }
+  }
+  if (RPB > 1) return;
+  if (S == 1 || !on) {
+    if (wave == 0 && s == 0) position_done(rows, f, ws, r, term);
     return;
   }
-  const int x = in.x;
-  auto emit = [&](int idx, const uint4& z, const uint4& zr) {
-    grad_vec<DT, ENT, REF>(z, zr, k, g);
-    if (idx == x / EPV) {
+  if (sh.role != kSettles) return;
+  // ---- the slices that have ended without their results
+  if (wave == 0) {
+    uint64_t left = __ballot(found == kLeft);
+    if (lane == 0) sh.left = left;
+    if (found == kLeft) {
 #pragma unroll
-      for (int i = 0; i < EPV; ++i) g[i] += idx * EPV + i == x ? k.a : 0.f;
+      for (int n = 0; n < kResultWords; ++n)
+        __hip_atomic_store(results + lane * kResultWords + n, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    store_grad<DT>(out, idx, V, g);
-  };
-#pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    const int idx = tid + j * T;
-    if (idx < nv) emit(idx, v[j], REF ? q[j % kRefAhead] : v[j]);
-    if (REF && j + kRefAhead < NB) q[j % kRefAhead] = load(ref, j + kRefAhead);
   }
-  for (int idx = tid + NB * T; idx < nv; idx += T) {
-    const uint4 z = load_vec_of<DT>(row, idx, V);
-    emit(idx, z, REF ? load_vec_of<DT>(ref, idx, V) : z);
+  __syncthreads();
+  for (uint64_t left = sh.left; __builtin_expect(left != 0, 0); left &= left - 1) {
+    const int other = __ffsll((long long)left) - 1, u0 = min(other * chunk, nv), u1 = min(u0 + chunk, nv);
+#pragma unroll 1
+    for (int idx = u0 + tid; idx < u1; idx += TR) {
+      const uint4 z = load_vec_of<DT>(row, idx, V);
+      emit_vec<DT, REF>(out, idx, V, x, z, REF ? load_vec_of<DT>(ref, idx, V) : z, k, ent);
+    }
   }
   if (wave == 0) position_done(rows, f, ws, r, term);
+}
+
+}  // namespace
+
+namespace {
+
+// How k_loss_join cuts rows of nv vectors: wavefronts per row, vectors in registers per thread, slices (0: too long) and vectors per slice.
+//  * Few rows: as many slices of a workgroup of four wavefronts as are resident together.
+//  * Many short rows: as few wavefronts per row as hold it, with as few registers as it takes (rows of 2000 bf16, four wavefronts
+//    each / one / one of few registers: 200000 rows 1463 / 703 / 536 us; of 8000, four / two / one: 50000 rows 529 / 369 / 364).
+//  * Many long rows: eight wavefronts of 8 vectors per thread, three workgroups per compute unit.  Bytes on their way are what the
+//    chip's rate takes, and a workgroup asks for nothing while it exchanges sums and settles, so that several should take turns.
+//    8192 rows of 128256 bf16, workgroups of 4 wavefronts x 16 vectors / 4 x 8 / 8 x 16 / 8 x 8 / 16 x 16 (no slices): 828 / 804 / 864 / 800 / 808 us;
+//    2048 of which 0.7 count 188 / 183 / 197 / 186 / 200; 2624 rows of 152064 331 / 326 / 366 / 311 / 427.
+//  * With a reference's row, twice the registers: four wavefronts of 8 + 8 vectors (1024 rows of 152064 bf16, 4 x (4 + 4) / 4 x (8 + 8) /
+//    8 x (8 + 8): 314 / 251 / 267 us), eight where they hold the row (12480 rows of 32000 bf16 508 us, two slices 540).
+struct JoinPlan {
+  int wpr, nb, S, chunk;
+};
+JoinPlan join_plan(int n, int nv, bool ref) {
+  const int most = ref ? 8 : 16;
+  if (n > kJoinResident) {
+    for (int nb = most / 4; nb <= most; nb *= 2)
+      if (nv <= 64 * nb) return {1, nb, 1, nv};
+    if (nv <= 128 * most) return {2, most, 1, nv};
+    if (ref && nv <= 256 * most) return {4, most, 1, nv};
+    if (nv <= 512 * 8) return {8, 8, 1, nv};
+    const int wpr = ref ? 4 : 8, S = (nv + 512 * wpr - 1) / (512 * wpr);
+    return {wpr, 8, S <= kMaxSplit ? S : 0, slice_chunk(nv, S)};
+  }
+  for (int turns = 1; turns <= most; ++turns) {
+    const int S = (nv + turns * kBlock - 1) / (turns * kBlock);
+    if (S <= kMaxSplit && (turns == most || (int64_t)S * n <= kJoinResident)) return {4, most, S, slice_chunk(nv, S)};
+  }
+  return {4, most, 0, 0};
 }
 
 }  // namespace
@@ -506,44 +692,47 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
   const int n = rows.n, epv = dt == ADASD_BF16 ? 8 : 4, nv = (rows.V + epv - 1) / epv;
   const bool ref = rows.ref.base != nullptr, ent = f.kind == kPolicy ? f.entropy_coef != 0.f : f.kind == kLogprob && f.dentropy;
   const bool by_ref = ref && f.kl_coef != 0.f;
-  const bool fused = rows.g.base && f.kind != kPreference && ref == by_ref && n >= 256;
+  const bool grad = rows.g.base != nullptr, own_row = grad && f.kind != kPreference && ref == by_ref;
   const dim3 block(kBlock);
-  f.adds_up = f.loss && n > 0 && n <= kAddsUp;
-  if (fused) {
-    const int T = nv <= 128 * 16 ? 128 : nv <= 256 * 16 ? 256 : nv <= 512 * 16 ? 512 : 1024;
-#define ADASD_FUSED_CASE(DTV, ENTV, REFV, TV, NBV) \
-    if (dt == DTV && ent == ENTV && ref == REFV && T == TV) \
-      launch_kernel((k_loss_fused<DTV, ENTV, REFV, TV, NBV>), dim3(n), dim3(TV), st, rows, f, ws);
-#define ADASD_FUSED_CASES(TV, NBV) \
-    ADASD_FUSED_CASE(ADASD_BF16, false, false, TV, NBV) ADASD_FUSED_CASE(ADASD_BF16, true, false, TV, NBV) \
-    ADASD_FUSED_CASE(ADASD_F32, false, false, TV, NBV) ADASD_FUSED_CASE(ADASD_F32, true, false, TV, NBV) \
-    ADASD_FUSED_CASE(ADASD_BF16, false, true, TV, NBV) ADASD_FUSED_CASE(ADASD_BF16, true, true, TV, NBV) \
-    ADASD_FUSED_CASE(ADASD_F32, false, true, TV, NBV) ADASD_FUSED_CASE(ADASD_F32, true, true, TV, NBV)
-    ADASD_FUSED_CASES(128, 16) ADASD_FUSED_CASES(256, 16) ADASD_FUSED_CASES(512, 16) ADASD_FUSED_CASES(1024, 16)
-#undef ADASD_FUSED_CASES
-#undef ADASD_FUSED_CASE
+  const JoinPlan plan = join_plan(n, nv, ref);
+  const bool join = n > 0 && plan.S > 0 && (plan.S == 1 || (int64_t)plan.S * n <= ws.slices) && (own_row || plan.wpr < 4);
+  f.adds_up = f.loss && n > 0 && (join ? plan.wpr >= kWaves && n <= kJoinAddsUp : n <= kAddsUp);
+  if (join) {
+    LossRows some = rows;
+    if (!own_row) some.g = RowPlace{};
+    const unsigned groups = plan.wpr >= kWaves ? n * plan.S : (n + kWaves / plan.wpr - 1) / (kWaves / plan.wpr);
+#define ADASD_JOIN_CASE(DTV, REFV, NBV, WPRV) \
+    if (dt == DTV && ref == REFV && plan.nb == NBV && plan.wpr == WPRV) \
+      launch_kernel((k_loss_join<DTV, REFV, NBV, WPRV>), dim3(groups), dim3(WPRV > kWaves ? 64 * WPRV : kBlock), st, some, f, plan.S, \
+                    plan.chunk, ent ? 1 : 0, ws);
+#define ADASD_JOIN_CASES(REFV, NBV, WPRV) ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV)
+    ADASD_JOIN_CASES(false, 4, 1) ADASD_JOIN_CASES(false, 8, 1) ADASD_JOIN_CASES(false, 16, 1) ADASD_JOIN_CASES(false, 16, 2)
+    ADASD_JOIN_CASES(false, 16, 4) ADASD_JOIN_CASES(false, 8, 8)
+    ADASD_JOIN_CASES(true, 2, 1) ADASD_JOIN_CASES(true, 4, 1) ADASD_JOIN_CASES(true, 8, 1) ADASD_JOIN_CASES(true, 8, 2)
+    ADASD_JOIN_CASES(true, 8, 4) ADASD_JOIN_CASES(true, 8, 8)
+#undef ADASD_JOIN_CASES
+#undef ADASD_JOIN_CASE
   } else if (n > 0) {
     const int S = scan_split(n, rows.V, dt), chunk = slice_chunk(nv, S);
 #define ADASD_LOSS_CASE(DTV, REFV) \
     if (dt == DTV && ref == REFV) launch_kernel((k_loss_sums<DTV, REFV>), dim3(n * S), block, st, rows, f, S, chunk, ws);
     ADASD_LOSS_CASE(ADASD_BF16, false) ADASD_LOSS_CASE(ADASD_BF16, true) ADASD_LOSS_CASE(ADASD_F32, false) ADASD_LOSS_CASE(ADASD_F32, true)
 #undef ADASD_LOSS_CASE
-    if (f.kind == kPreference && !f.adds_up) launch_kernel(k_loss_pairs, dim3(f.P), dim3(64), st, f, rows.T, ws);
-    if (rows.g.base) {
-      const int turns = 8, slices = (nv + turns * kBlock - 1) / (turns * kBlock);
-      const dim3 pieces(n, slices);
-#define ADASD_GRAD_CASE(DTV, ENTV, REFV) \
-      if (dt == DTV && ent == ENTV && by_ref == REFV) \
-        launch_kernel((k_loss_grad<DTV, ENTV, REFV>), pieces, block, st, rows, slices, ws, f.kind == kPreference ? 1 : 0);
-      ADASD_GRAD_CASE(ADASD_BF16, false, false) ADASD_GRAD_CASE(ADASD_BF16, false, true) ADASD_GRAD_CASE(ADASD_BF16, true, false)
-      ADASD_GRAD_CASE(ADASD_BF16, true, true) ADASD_GRAD_CASE(ADASD_F32, false, false) ADASD_GRAD_CASE(ADASD_F32, false, true)
-      ADASD_GRAD_CASE(ADASD_F32, true, false) ADASD_GRAD_CASE(ADASD_F32, true, true)
+  }
+  if (f.kind == kPreference && n > 0 && !f.adds_up) launch_kernel(k_loss_pairs, dim3(f.P), dim3(64), st, f, rows.T, ws);
+  if (grad && n > 0 && !(join && own_row)) {
+    const int per = max(kPiece, ((nv + kMostPieces - 1) / kMostPieces + 63) / 64 * 64), pieces = (nv + per - 1) / per;
+    const uint32_t groups = ((uint32_t)n * (uint32_t)pieces + kWaves - 1) / kWaves;
+    const dim3 grid(groups < kMostGroups ? groups : kMostGroups);
+#define ADASD_GRAD_CASE(DTV, REFV) \
+    if (dt == DTV && by_ref == REFV) \
+      launch_kernel((k_loss_grad<DTV, REFV>), grid, block, st, rows, pieces, per, ws, f.kind == kPreference ? 1 : 0, ent ? 1 : 0);
+    ADASD_GRAD_CASE(ADASD_BF16, false) ADASD_GRAD_CASE(ADASD_BF16, true) ADASD_GRAD_CASE(ADASD_F32, false) ADASD_GRAD_CASE(ADASD_F32, true)
 #undef ADASD_GRAD_CASE
-    }
   }
   if (f.loss && !f.adds_up) {
     const bool pairs = f.kind == kPreference;
-    launch_kernel(k_loss_total, dim3(1), dim3(64), st, (const double*)(pairs ? ws.pair : ws.term), n == 0 ? 0 : pairs ? f.P : n, f.loss);
+    launch_kernel(k_loss_total, dim3(1), dim3(64), st, pairs ? ws.pair : ws.term, n == 0 ? 0 : pairs ? f.P : n, f.loss);
   }
   return hipGetLastError();
 }

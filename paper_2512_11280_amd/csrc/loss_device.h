@@ -19,19 +19,12 @@ struct LossSums {          // of a slice
 };
 __device__ __forceinline__ LossSums loss_empty() { return LossSums{kNegHuge, 0.f, 0.f, 0.f, kNegHuge, 0.f}; }
 
-// One vector of the row (and of the reference's) joins a lane's sums, about the reference m that the sums have (mr follows).  The vector's sums are
+// One vector of the row (and of the reference's) joins a lane's sums, about the references that the sums have.  The vector's sums are
 // formed on their own, so that a chain of additions is one per vector long.
 template <int DT, bool REF>
 __device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const uint4& xr, float c) {
   constexpr int EPV = Elem<DT>::per_vec;
-  const float neg_m = -a.m;
-  if (REF) {
-    const uint4 other[1] = {xr};
-    const float mr = fmaxf(a.mr, vecs_max<DT, 1>(other));
-    a.sr *= ex2(a.mr - mr);
-    a.mr = mr;
-  }
-  const float neg_mr = -a.mr;
+  const float neg_m = -a.m, neg_mr = -a.mr;
   float s[2] = {0.f, 0.f}, u[2] = {0.f, 0.f}, w[2] = {0.f, 0.f}, sr[2] = {0.f, 0.f};
 #pragma unroll
   for (int g = 0; g < EPV / 4; ++g) {
@@ -67,21 +60,52 @@ __device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const 
   }
 }
 
-// The sums about a reference that is at least `top`.
-__device__ __forceinline__ void loss_raise(LossSums& a, float top) {
-  const float m = fmaxf(a.m, top), d = a.m - m, f = ex2(d);
+// The sums about references that are at least as large as the logits of NV more vectors.
+template <int DT, bool REF, int NV>
+__device__ __forceinline__ void loss_raise(LossSums& a, const uint4 (&x)[NV], const uint4 (&xr)[NV]) {
+  const float m = fmaxf(a.m, vecs_max<DT, NV>(x)), d = a.m - m, f = ex2(d);
   a.u = (a.u + d * a.s) * f;
   a.s *= f;
-  a.w *= f;
   a.m = m;
+  if (REF) {
+    a.w *= f;
+    const float mr = fmaxf(a.mr, vecs_max<DT, NV>(xr));
+    a.sr *= ex2(a.mr - mr);
+    a.mr = mr;
+  }
 }
-template <int DT, bool REF>
-__device__ __forceinline__ void loss_push(LossSums& a, const uint4& x, const uint4& xr, float c) {
-  const uint4 one[1] = {x};
-  loss_raise(a, vecs_max<DT, 1>(one));
-  loss_push_at<DT, REF>(a, x, xr, c);
+// Sums of two parts of a row, about the larger references.
+template <bool REF> __device__ __forceinline__ LossSums loss_merge(const LossSums& a, const LossSums& b) {
+  LossSums r;
+  r.m = fmaxf(a.m, b.m);
+  const float da = a.m - r.m, db = b.m - r.m, fa = ex2(da), fb = ex2(db);
+  r.s = a.s * fa + b.s * fb;
+  r.u = (a.u + da * a.s) * fa + (b.u + db * b.s) * fb;
+  r.w = 0.f;
+  r.mr = kNegHuge;
+  r.sr = 0.f;
+  if (REF) {
+    r.w = a.w * fa + b.w * fb;
+    r.mr = fmaxf(a.mr, b.mr);
+    r.sr = a.sr * ex2(a.mr - r.mr) + b.sr * ex2(b.mr - r.mr);
+  }
+  return r;
 }
 
+// The same sums about references whose lowest bit is set (the flag of the hand-off words).
+template <bool REF> __device__ __forceinline__ LossSums loss_flagged(const LossSums& a) {
+  LossSums r = a;
+  r.m = __uint_as_float(__float_as_uint(a.m) | 1u);
+  const float d = a.m > kNegHuge ? a.m - r.m : 0.f, f = ex2(d);
+  r.s = a.s * f;
+  r.u = (a.u + d * a.s) * f;
+  if (REF) {
+    r.w = a.w * f;
+    r.mr = __uint_as_float(__float_as_uint(a.mr) | 1u);
+    r.sr = a.sr * ex2(a.mr > kNegHuge ? a.mr - r.mr : 0.f);
+  }
+  return r;
+}
 // One wavefront folds its lanes' sums; uniform results, about references whose lowest bit is set (it is the flag of the hand-off words).
 template <bool REF> __device__ __forceinline__ LossSums loss_fold_wave(const LossSums& a) {
   LossSums r = a;

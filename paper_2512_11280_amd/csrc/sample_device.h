@@ -117,8 +117,10 @@ struct PlainWords {
 struct Arrivals {
   int32_t* base;
   int len, row, rows;
+  bool sets = false;       // a set for each row of a launch of many, next to one another, too: their last slices then wait as those of few rows do
+  __device__ __forceinline__ bool waits() const { return sets || few_rows(rows); }
   __device__ __forceinline__ int32_t* count() const { return base + row * ticket_stride(rows, len); }                // (many rows)
-  __device__ __forceinline__ uint64_t* set() const { return reinterpret_cast<uint64_t*>(base + row * 32); }          // (few rows)
+  __device__ __forceinline__ uint64_t* set() const { return reinterpret_cast<uint64_t*>(base + (sets ? 2 * (size_t)row : (size_t)row * 32)); }   // (few rows)
 };
 static_assert(kFewRows * 32 <= kTicket1Len && kFewRows * 32 <= kTicket3Len, "a line of 128 bytes for each of few rows");
 // (lane 0 adds 1; what the word held before, in every lane)
@@ -175,9 +177,9 @@ __device__ __forceinline__ bool hand_off(const Slots& slots, int s, int S, const
   const uint64_t w0 = w[0], w1 = w[1], w2 = w[2], word = lane == 0 ? w0 : lane == 1 ? w1 : w2;
   static_assert(kXchgWords == 3, "a lane per word");
   if (lane < kXchgWords) __hip_atomic_store(slots.at(s) + lane, word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const bool may_give_up = few_rows(a.rows) && s == S - 1;
+  const bool may_give_up = a.waits() && s == S - 1;
   if (!may_give_up) {
-    if (!few_rows(a.rows)) {
+    if (!a.waits()) {
       if (!last_to_add(add_arrival(a.count()), S)) return false;
       set_arrival(a.count(), 0);
     } else {

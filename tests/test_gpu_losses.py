@@ -472,3 +472,82 @@ def test_a_training_step_on_verified_tokens(am, dtype):
     loss.backward()
     assert abs(loss.item() - p.loss.item()) < 2e-5
     assert (W.grad.double() - Wd.grad).norm() < bound * Wd.grad.norm()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_rows_of_every_cut(am, dtype):
+    """One to four wavefronts per row, a workgroup per row, slices; with as many rows as make the cuts differ."""
+    for B, T, V in ((43, 31, 40), (29, 45, 2003), (27, 48, 4009), (53, 25, 6007), (21, 63, 9001)):     # above 1280 rows
+        c = Case(B, T, V, dtype, seed=18)
+        _policy(am, c, "full", 0.01)
+        _policy(am, c, "none", 0.01)
+    c = Case(2, 667, 2003, dtype, seed=19)
+    _preference(am, c)
+    act = (c.w != 0).to(torch.uint8)
+    lp, H, st = am.token_logprob(c.z.cuda(), c.x.cuda(), c.ws(am), active=act.cuda())
+    o = R.rows(c.z, c.x)
+    R.near(lp, torch.where(act.bool(), o["lp"], 0.0), R.tol_lp(o), "logprob")
+    R.near(H, torch.where(act.bool(), o["H"], 0.0), R.tol_H(o), "entropy")
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("V", [300001, 1100003])
+def test_long_vocabularies(am, V, dtype):
+    """Rows of more slices than there are records in a wavefront's lanes, and nearly so."""
+    c = Case(1, 3, V, dtype, seed=20, masked=0.0)
+    _policy(am, c, "full", 0.01)
+    _policy(am, c, "sampled")
+    c = Case(2, 2, V, dtype, seed=21)
+    _preference(am, c)
+
+
+def test_many_positions(am):
+    """More positions than the last one adds up by itself; pairs as many and as long."""
+    c = Case(70, 71, 33, BF, seed=22)
+    _policy(am, c, "sampled", 0.01)
+    _preference(am, c)
+    c = Case(2, 2600, 33, F, seed=23)
+    _policy(am, c)
+    _preference(am, c)
+    c = Case(5200, 1, 33, F, seed=24)
+    _preference(am, c)
+
+
+@pytest.mark.parametrize("how", ["unarrived", "given_up"])
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_slices_whose_records_are_not_waited_for(am, how, dtype):
+    """The same results (to the last bits) where no slice waits for the others' sums, or all count as not there; and the next call finds
+    the workspace as it should be."""
+    import ctypes
+    from test_losses import _Rows
+    lib = am.load_library()
+    for B, T, V in ((1, 1, 128256), (3, 5, 32003), (2, 40, 70001), (1, 700, 20011)):
+        c = Case(B, T, V, dtype, seed=25)
+        z, x, ws = c.z.cuda(), c.x.cuda(), c.ws(am)
+        o = R.rows(c.z, c.x)
+        a, h = c.n(B, T), c.n(B, T)
+        for again in range(2):
+            lp, H = (torch.full((B, T), 9.0, device="cuda") for _ in range(2))
+            st = torch.full((B, T), 9, dtype=torch.int32, device="cuda")
+            g = torch.full_like(z, 9.0)
+            rows = _Rows(z.data_ptr(), int(dtype == BF), B, T, V, z.stride(0), z.stride(1), x.data_ptr())
+            rows.logprob, rows.entropy, rows.status = lp.data_ptr(), H.data_ptr(), st.data_ptr()
+            rows.workspace, rows.ws_bytes = ws.ptr, ws.bytes
+            s = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+            assert getattr(lib, f"adasd_test_logprob_{how}")(ctypes.byref(rows), s) == 0
+            R.near(lp, o["lp"], R.tol_lp(o), "logprob")
+            R.near(H, o["H"], R.tol_H(o), "entropy")
+            assert not st.any()
+            # (records that count as not there are formed from the logits again, which have to be whole then: not in place)
+            for out in (g,) if how == "unarrived" else (g, z.clone()):
+                if out is not g:
+                    z2 = out
+                    rows.logits = z2.data_ptr()
+                rows.dlogits, rows.d_seq_stride, rows.d_pos_stride = out.data_ptr(), out.stride(0), out.stride(1)
+                da, dh = a.cuda(), h.cuda()
+                f = getattr(lib, f"adasd_test_logprob_grad_{how}")
+                assert f(ctypes.byref(rows), ctypes.c_void_p(da.data_ptr()), ctypes.c_void_p(dh.data_ptr()), s) == 0
+                torch.cuda.synchronize()
+                R.near(out, *R.grad(o, a, h, dtype=dtype), "dlogits")
+            rows.logits = z.data_ptr()
+            assert torch.equal(am.token_logprob_grad(z, x, ws, a.cuda(), h.cuda()), am.token_logprob_grad(z, x, c.ws(am), a.cuda(), h.cuda()))
