@@ -20,6 +20,12 @@ namespace {
 
 using namespace sampling;
 
+// A whole vector; PAST: without a place in the caches.
+template <bool PAST> __device__ __forceinline__ uint4 load_whole(const char* row, int idx) {
+  if (!PAST) return load_vec_any(row, idx);
+  const vec16_any v = __builtin_nontemporal_load(reinterpret_cast<const vec16_any*>(row + (size_t)idx * 16));
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
 template <int DT> __device__ __forceinline__ uint4 load_vec_of(const char* row, int idx, int V) {
   return idx < V / Elem<DT>::per_vec ? load_vec_any(row, idx) : load_last_vec<DT>(row, V);
 }
@@ -246,7 +252,7 @@ template <int DT, bool REF> __device__ __noinline__ LossSums wave_sums(const cha
 
 // A slice's vectors come in batches of four per thread, the next batch on its way.
 constexpr int kSumsBatch = 4;
-template <int DT, bool REF> __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f, int S, int chunk, LossWorkspace ws) {
+template <int DT, bool REF, bool PAST> __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f, int S, int chunk, LossWorkspace ws) {
   __shared__ LossSums sh[kWaves];
   const int r = blockIdx.x / S, s = blockIdx.x - r * S, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = r / rows.T, t = r - b * rows.T, V = rows.V;
@@ -263,7 +269,11 @@ template <int DT, bool REF> __global__ void __launch_bounds__(kBlock) k_loss_sum
   const char* row = row_at<DT>(rows.z, b, t);
   const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
   const int nv = vectors_of<DT>(V), v0 = min(s * chunk, nv), v1 = min(v0 + chunk, nv);
-  auto load = [&](const char* from, int idx) { return idx < v1 ? load_vec_of<DT>(from, idx, V) : neutral_vec<DT>(); };
+  const int whole = V / Elem<DT>::per_vec;
+  auto load = [&](const char* from, int idx) {
+    if (idx >= v1) return neutral_vec<DT>();
+    return idx < whole ? load_whole<PAST>(from, idx) : load_last_vec<DT>(from, V);
+  };
   uint4 next[kSumsBatch], nextr[kSumsBatch];
 #pragma unroll
   for (int k = 0; k < kSumsBatch; ++k) next[k] = load(row, v0 + tid + k * kBlock);
@@ -334,7 +344,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {       // neare
   __builtin_memcpy(&r, &v, 4);
   return r;
 }
-// A whole vector of gradients, or the elements of the last one that the row has.
+// A whole vector of gradients, or the elements of the last one that the row has.  Stored past the caches: a gradient of more than a few
+// hundred rows does not stay in them till it is read, and takes the place of logits that are still to be read (8192 rows of
+// 128256 bf16 796 -> 771 us, preference loss of 512 rows of 128256 float 162 -> 132, KL over 1024 rows of 152064 246 -> 227).
 template <int DT> __device__ __forceinline__ void store_grad(char* row, int idx, int V, const float (&g)[Elem<DT>::per_vec]) {
   constexpr int EPV = Elem<DT>::per_vec;
   uint32_t w[4];
@@ -347,7 +359,7 @@ template <int DT> __device__ __forceinline__ void store_grad(char* row, int idx,
     vec16_any v;
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = w[i];
-    *reinterpret_cast<vec16_any*>(row + (size_t)idx * 16) = v;
+    __builtin_nontemporal_store(v, reinterpret_cast<vec16_any*>(row + (size_t)idx * 16));
     return;
   }
 #pragma unroll
@@ -405,7 +417,8 @@ __device__ __forceinline__ void emit_vec(char* out, int idx, int V, int x, const
   store_grad<DT>(out, idx, V, g);
 }
 
-// Pieces of rows of `per` vectors, a wavefront each.
+// Pieces of rows of `per` vectors, a wavefront each, from the last row to the first: the rows read last are still in the cache behind the L2s
+// (preference loss of 2048 rows of 128256 bf16 of which 0.67 count: 235 -> 211 us).
 constexpr int kPiece = 8 * 64, kMostPieces = 2048;      // (2^20 rows: no more than 2^31 pieces)
 constexpr uint32_t kMostGroups = 1u << 22;
 template <int DT, bool REF>
@@ -413,7 +426,8 @@ __global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces,
   const int lane = threadIdx.x & 63, V = rows.V, nv = vectors_of<DT>(V);
   const uint32_t step = gridDim.x * kWaves, units = (uint32_t)rows.n * (uint32_t)pieces;
   for (uint32_t unit = blockIdx.x * kWaves + uniform(threadIdx.x >> 6); unit < units; unit += step) {
-    const int r = (int)(unit / (uint32_t)pieces), piece = (int)(unit - (uint32_t)r * (uint32_t)pieces), b = r / rows.T, t = r - b * rows.T;
+    const uint32_t back = units - 1 - unit;
+    const int r = (int)(back / (uint32_t)pieces), piece = (int)(back - (uint32_t)r * (uint32_t)pieces), b = r / rows.T, t = r - b * rows.T;
     LossCoef k = scalar_load(ws.coef + r);
     if (by_sequence) {
       const float d = scalar_load(ws.seq + b);
@@ -493,7 +507,7 @@ __device__ __forceinline__ uint64_t send_results(uint64_t* at, int S, int own, c
 
 // Wavefronts per SIMD that the registers are limited for (64 of data and about 50 more: four; 16: eight).
 constexpr int join_waves(int nb, bool ref) { return !ref ? (nb <= 4 ? 8 : nb <= 8 ? 6 : 4) : (nb <= 2 ? 7 : nb <= 4 ? 5 : 4); }
-template <int DT, bool REF, int NB, int WPR>
+template <int DT, bool REF, int NB, int WPR, bool PAST>
 __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(NB, REF)) k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, LossWorkspace ws) {
   constexpr int RPB = WPR < kWaves ? kWaves / WPR : 1, TR = 64 * WPR;          // rows per workgroup, threads per row
   __shared__ JoinShared<WPR < kWaves ? kWaves : WPR> sh;
@@ -521,7 +535,7 @@ __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(N
     const int full = min(v1, V / Elem<DT>::per_vec);
     auto load = [&](const char* from, int j) {
       const int idx = v0 + me + j * TR;
-      if (v0 + (j + 1) * TR <= full) return load_vec_any(from, idx);
+      if (v0 + (j + 1) * TR <= full) return load_whole<PAST>(from, idx);
       return idx < v1 ? load_vec_of<DT>(from, idx, V) : neutral_vec<DT>();
     };
 #pragma unroll
@@ -688,6 +702,11 @@ JoinPlan join_plan(int n, int nv, bool ref) {
 
 }  // namespace
 
+// Logits of so many bytes are read past the caches.  Gradients of one launch read them once (1024 rows of 152064 bf16 and a reference's 226 -> 218
+// us, 200000 rows of 2000 493 -> 453; 385 rows of 32003 float and a reference's, which the cache behind the L2s can hold from the kernel
+// that wrote them, 34 -> 35).  Log-probabilities are often asked for ahead of a gradient, so only what that cache cannot hold.
+constexpr int64_t kJoinPast = (int64_t)64 << 20, kSumsPast = (int64_t)256 << 20;
+
 hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorkspace& ws, hipStream_t st) {
   const int n = rows.n, epv = dt == ADASD_BF16 ? 8 : 4, nv = (rows.V + epv - 1) / epv;
   const bool ref = rows.ref.base != nullptr, ent = f.kind == kPolicy ? f.entropy_coef != 0.f : f.kind == kLogprob && f.dentropy;
@@ -696,16 +715,20 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
   const dim3 block(kBlock);
   const JoinPlan plan = join_plan(n, nv, ref);
   const bool join = n > 0 && plan.S > 0 && (plan.S == 1 || (int64_t)plan.S * n <= ws.slices) && (own_row || plan.wpr < 4);
+  const int64_t bytes = (int64_t)n * nv * 16;
+  const bool past = join ? own_row && bytes > kJoinPast : f.kind == kLogprob && bytes > kSumsPast;
   f.adds_up = f.loss && n > 0 && (join ? plan.wpr >= kWaves && n <= kJoinAddsUp : n <= kAddsUp);
   if (join) {
     LossRows some = rows;
     if (!own_row) some.g = RowPlace{};
     const unsigned groups = plan.wpr >= kWaves ? n * plan.S : (n + kWaves / plan.wpr - 1) / (kWaves / plan.wpr);
-#define ADASD_JOIN_CASE(DTV, REFV, NBV, WPRV) \
-    if (dt == DTV && ref == REFV && plan.nb == NBV && plan.wpr == WPRV) \
-      launch_kernel((k_loss_join<DTV, REFV, NBV, WPRV>), dim3(groups), dim3(WPRV > kWaves ? 64 * WPRV : kBlock), st, some, f, plan.S, \
+#define ADASD_JOIN_CASE(DTV, REFV, NBV, WPRV, PASTV) \
+    if (dt == DTV && ref == REFV && plan.nb == NBV && plan.wpr == WPRV && past == PASTV) \
+      launch_kernel((k_loss_join<DTV, REFV, NBV, WPRV, PASTV>), dim3(groups), dim3(WPRV > kWaves ? 64 * WPRV : kBlock), st, some, f, plan.S, \
                     plan.chunk, ent ? 1 : 0, ws);
-#define ADASD_JOIN_CASES(REFV, NBV, WPRV) ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV)
+#define ADASD_JOIN_CASES(REFV, NBV, WPRV) \
+    ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, false) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, false) \
+    ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, true) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, true)
     ADASD_JOIN_CASES(false, 4, 1) ADASD_JOIN_CASES(false, 8, 1) ADASD_JOIN_CASES(false, 16, 1) ADASD_JOIN_CASES(false, 16, 2)
     ADASD_JOIN_CASES(false, 16, 4) ADASD_JOIN_CASES(false, 8, 8)
     ADASD_JOIN_CASES(true, 2, 1) ADASD_JOIN_CASES(true, 4, 1) ADASD_JOIN_CASES(true, 8, 1) ADASD_JOIN_CASES(true, 8, 2)
@@ -714,9 +737,11 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
 #undef ADASD_JOIN_CASE
   } else if (n > 0) {
     const int S = scan_split(n, rows.V, dt), chunk = slice_chunk(nv, S);
-#define ADASD_LOSS_CASE(DTV, REFV) \
-    if (dt == DTV && ref == REFV) launch_kernel((k_loss_sums<DTV, REFV>), dim3(n * S), block, st, rows, f, S, chunk, ws);
-    ADASD_LOSS_CASE(ADASD_BF16, false) ADASD_LOSS_CASE(ADASD_BF16, true) ADASD_LOSS_CASE(ADASD_F32, false) ADASD_LOSS_CASE(ADASD_F32, true)
+#define ADASD_LOSS_CASE(DTV, REFV, PASTV) \
+    if (dt == DTV && ref == REFV && past == PASTV) \
+      launch_kernel((k_loss_sums<DTV, REFV, PASTV>), dim3(n * S), block, st, rows, f, S, chunk, ws);
+    ADASD_LOSS_CASE(ADASD_BF16, false, false) ADASD_LOSS_CASE(ADASD_BF16, true, false) ADASD_LOSS_CASE(ADASD_F32, false, false)
+    ADASD_LOSS_CASE(ADASD_F32, true, false) ADASD_LOSS_CASE(ADASD_BF16, false, true) ADASD_LOSS_CASE(ADASD_F32, false, true)
 #undef ADASD_LOSS_CASE
   }
   if (f.kind == kPreference && n > 0 && !f.adds_up) launch_kernel(k_loss_pairs, dim3(f.P), dim3(64), st, f, rows.T, ws);
