@@ -72,6 +72,21 @@ __device__ __forceinline__ double log2_fine(float x) {
   return (double)e + (2.0 / 0.693147180559945309417232) * f * p;
 }
 
+// ln(1 + x), 0 <= x <= 1, to about 1e-11: 2 (f + f^3/3 + ...), f = x / (2 + x) <= 1/3.
+__device__ __forceinline__ double log1p_fine(double x) {
+  const double f = x / (2.0 + x), g = f * f;
+  double p = 1.0 / 21;
+  p = fma(p, g, 1.0 / 19);
+  p = fma(p, g, 1.0 / 17);
+  p = fma(p, g, 1.0 / 15);
+  p = fma(p, g, 1.0 / 13);
+  p = fma(p, g, 1.0 / 11);
+  p = fma(p, g, 1.0 / 9);
+  p = fma(p, g, 1.0 / 7);
+  p = fma(p, g, 1.0 / 5);
+  p = fma(p, g, 1.0 / 3);
+  return 2.0 * fma(p * g, f, f);
+}
 // e^d - 1 to about 1e-14 relative, whatever the size of d: e^d = 2^k e^r, |r| <= ln 2 / 2, and the series of e^r - 1.
 __device__ __forceinline__ double expm1_fine(double d) {
   const double k = rint(fmin(fmax(d, -800.0), 800.0) * 1.44269504088896340736);

@@ -221,7 +221,7 @@ struct LossWorkspace {
   int32_t* ticket;      // [kTicketLossLen] arrival words of the rows that k_loss_sums cuts into slices (see Arrivals), zero between launches
   int32_t* sets;        // [positions][2] the same of k_loss_join
   int32_t* done;        // [32 + kAddsUp] positions (or pairs) that are done, and positions of each pair; zero between launches
-  double* fresh;        // [kAddsUp + kAddsUp / 2] terms of positions, and of pairs, that the last one done adds up; zero between launches
+  double* fresh;        // [kAddsUp] terms of positions that the last one done adds up; zero between launches
   uint64_t* xchg;       // [slices][kXchgWords + kResultWords] hand-off words, zero between launches
   LossCoef* coef;       // [positions]
   double* term;         // [positions] what a position adds to the loss or to its sequence's score (of more than kAddsUp)

@@ -139,18 +139,27 @@ __device__ __forceinline__ void report_nothing(const LossRows& rows, const LossT
 // say themselves that they are there (the lowest bit of the fraction is set; a cleared word is 0), and are cleared as they are read.  The
 // order of the additions is the same either way.
 __device__ __forceinline__ double flagged_term(double v) { return __longlong_as_double(__double_as_longlong(v) | 1ll); }
-template <bool FRESH> __device__ __forceinline__ double wave_total(double* v, int n) {
+template <bool FRESH, int M> __device__ __forceinline__ void wave_total_of(double* const (&v)[M], int n, double (&t)[M]) {
+  constexpr int U = 8 / M;
   const int lane = threadIdx.x & 63;
-  double t = 0.0;
-  for (int base = 0; base < n; base += 8 * 64) {
-    double x[8];
+#pragma unroll
+  for (int m = 0; m < M; ++m) t[m] = 0.0;
+  for (int base = 0; base < n; base += U * 64) {
+    double x[M][U];
     auto look = [&] {
       bool there = true;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int i = base + k * 64 + lane;
-        x[k] = i < n ? (FRESH ? ld_agent(v + i) : v[i]) : 0.0;
-        there = there && (i >= n || (__double_as_longlong(x[k]) & 1));
+      for (int m = 0; m < M; ++m) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const int i = base + k * 64 + lane;
+          x[m][k] = i < n ? (FRESH ? ld_agent(v[m] + i) : v[m][i]) : 0.0;
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) there = there && (base + k * 64 + lane >= n || (__double_as_longlong(x[m][k]) & 1));
       }
       return __all(there) != 0;
     };
@@ -158,21 +167,37 @@ template <bool FRESH> __device__ __forceinline__ double wave_total(double* v, in
     // (all had been sent when the last one was counted: this ends at once, unless calls that share a workspace have not been ordered)
     for (int polls = kWaitPolls; !there && polls > 0; --polls) there = look();
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      t += there ? x[k] : (double)NAN;
-      if (FRESH && base + k * 64 + lane < n) st_agent(v + base + k * 64 + lane, 0.0);
+    for (int m = 0; m < M; ++m) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        t[m] += there ? x[m][k] : (double)NAN;
+        if (FRESH && base + k * 64 + lane < n) st_agent(v[m] + base + k * 64 + lane, 0.0);
+      }
     }
   }
-  return wave_sum(t);
+#pragma unroll
+  for (int m = 0; m < M; ++m) t[m] = wave_sum(t[m]);
 }
-
-__device__ __forceinline__ double softplus(double v) { return fmax(v, 0.0) + log1p(exp(-fabs(v))); }
+template <bool FRESH> __device__ __forceinline__ double wave_total(double* v, int n) {
+  double* const p[1] = {v};
+  double t[1];
+  wave_total_of<FRESH, 1>(p, n, t);
+  return t[0];
+}
+template <bool FRESH> __device__ __forceinline__ void wave_totals(double* a, double* b, int n, double& ta, double& tb) {
+  double* const p[2] = {a, b};
+  double t[2];
+  wave_total_of<FRESH, 2>(p, n, t);
+  ta = t[0];
+  tb = t[1];
+}
 
 // A pair's loss and slope from the terms of its positions, by one wavefront (lane 0 writes).
 template <bool FRESH> __device__ __forceinline__ void settle_pair(const LossTerm& f, const LossWorkspace& ws, int i, int T) {
   const int P = f.P;
   double* terms = FRESH ? ws.fresh : ws.term;
-  const double chosen = wave_total<FRESH>(terms + (size_t)i * T, T), rejected = wave_total<FRESH>(terms + (size_t)(P + i) * T, T);
+  double chosen, rejected;
+  wave_totals<FRESH>(terms + (size_t)i * T, terms + (size_t)(P + i) * T, T, chosen, rejected);
   const double beta = (double)f.beta, e = (double)f.smoothing, D = chosen - rejected;
   double m, loss, slope;
   if (f.pair_kind == 1) {
@@ -186,18 +211,18 @@ template <bool FRESH> __device__ __forceinline__ void settle_pair(const LossTerm
       loss = fmax(1.0 - m, 0.0);
       slope = m < 1.0 ? -beta : 0.0;
     } else {
-      // (a part with factor 0 is left out: its logarithm may be infinite)
-      loss = (e < 1.0 ? (1.0 - e) * softplus(-m) : 0.0) + (e > 0.0 ? e * softplus(m) : 0.0);
-      slope = beta * (e / (1.0 + exp(-m)) - (1.0 - e) / (1.0 + exp(m)));
+      // ln(1 + e^(-m)) = max(-m, 0) + ln(1 + e^-|m|), and the same of m
+      const double E = expm1_fine(-fabs(m)) + 1.0, tail = log1p_fine(E), small = E / (1.0 + E), large = 1.0 / (1.0 + E);
+      // (a part with factor 0 is left out: it may be infinite)
+      loss = tail + (e < 1.0 ? (1.0 - e) * fmax(-m, 0.0) : 0.0) + (e > 0.0 ? e * fmax(m, 0.0) : 0.0);
+      slope = beta * (e * (m >= 0.0 ? large : small) - (1.0 - e) * (m >= 0.0 ? small : large));
     }
     if (m != m) loss = slope = m;
   }
   const double w = f.pair_weight ? (double)f.pair_weight[i] : 1.0 / (double)P;
   const double scale = w * (f.grad_scale ? (double)*f.grad_scale : 1.0);
   if ((threadIdx.x & 63) != 0) return;
-  const double part = w != 0.0 ? w * loss : 0.0;
-  if (FRESH) st_agent(ws.fresh + kAddsUp + i, flagged_term(part));
-  else ws.pair[i] = part;
+  ws.pair[i] = w != 0.0 ? w * loss : 0.0;
   ws.seq[i] = w != 0.0 ? (float)(scale * slope) : 0.f;
   ws.seq[P + i] = w != 0.0 ? (float)(-scale * slope) : 0.f;
   if (f.pair_loss) f.pair_loss[i] = (float)loss;
@@ -214,7 +239,7 @@ __device__ __forceinline__ bool last_of(int32_t* counter, int n) {
   set_arrival(counter, 0);
   return true;
 }
-// Position r is settled (one wavefront): the last of a pair settles the pair, the last of all adds up the loss.
+// Position r is settled (one wavefront): the last of a pair settles the pair; without pairs the last of all adds up the loss.
 __device__ __forceinline__ void position_done(const LossRows& rows, const LossTerm& f, const LossWorkspace& ws, int r, double term) {
   if (!f.loss) return;
   const bool first = (threadIdx.x & 63) == 0;
@@ -223,17 +248,13 @@ __device__ __forceinline__ void position_done(const LossRows& rows, const LossTe
     return;
   }
   if (first) st_agent(ws.fresh + r, flagged_term(term));
-  int n = rows.n;
-  double* v = ws.fresh;
   if (f.kind == kPreference) {
     const int b = r / rows.T, i = b < f.P ? b : b - f.P;
-    if (!last_of(ws.done + 32 + i * ticket_stride(f.P, kAddsUp), 2 * rows.T)) return;
-    settle_pair<true>(f, ws, i, rows.T);
-    n = f.P;
-    v += kAddsUp;
+    if (last_of(ws.done + 32 + i * ticket_stride(f.P, kAddsUp), 2 * rows.T)) settle_pair<true>(f, ws, i, rows.T);
+    return;
   }
-  if (!last_of(ws.done, n)) return;
-  const double t = wave_total<true>(v, n);
+  if (!last_of(ws.done, rows.n)) return;
+  const double t = wave_total<true>(ws.fresh, rows.n);
   if (first) *f.loss = (float)t;
 }
 
@@ -421,15 +442,22 @@ __device__ __forceinline__ void emit_vec(char* out, int idx, int V, int x, const
 // (preference loss of 2048 rows of 128256 bf16 of which 0.67 count: 235 -> 211 us).
 constexpr int kPiece = 8 * 64, kMostPieces = 2048;      // (2^20 rows: no more than 2^31 pieces)
 constexpr uint32_t kMostGroups = 1u << 22;
+constexpr int kResidentWaves = 8 * 4 * 256;
 template <int DT, bool REF>
-__global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces, int per, LossWorkspace ws, int by_sequence, int ent) {
+__global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces, int per, LossWorkspace ws, int P, float* loss, int ent) {
   const int lane = threadIdx.x & 63, V = rows.V, nv = vectors_of<DT>(V);
-  const uint32_t step = gridDim.x * kWaves, units = (uint32_t)rows.n * (uint32_t)pieces;
+  const uint32_t step = (gridDim.x - (loss ? 1u : 0u)) * kWaves, units = (uint32_t)rows.n * (uint32_t)pieces;
+  if (loss && blockIdx.x == gridDim.x - 1) {         // (the pairs' sum; its workgroup is one more than the rows take)
+    if (threadIdx.x >= 64) return;
+    const double total = wave_total<false>(ws.pair, P);
+    if (lane == 0) *loss = (float)total;
+    return;
+  }
   for (uint32_t unit = blockIdx.x * kWaves + uniform(threadIdx.x >> 6); unit < units; unit += step) {
     const uint32_t back = units - 1 - unit;
     const int r = (int)(back / (uint32_t)pieces), piece = (int)(back - (uint32_t)r * (uint32_t)pieces), b = r / rows.T, t = r - b * rows.T;
     LossCoef k = scalar_load(ws.coef + r);
-    if (by_sequence) {
+    if (P > 0) {                       // (a pair's slope, sequence by sequence)
       const float d = scalar_load(ws.seq + b);
       k.a = d == 0.f ? 0.f : k.a * d;
       k.k0 = d == 0.f ? 0.f : k.k0 * d;
@@ -744,19 +772,22 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
     ADASD_LOSS_CASE(ADASD_F32, true, false) ADASD_LOSS_CASE(ADASD_BF16, false, true) ADASD_LOSS_CASE(ADASD_F32, false, true)
 #undef ADASD_LOSS_CASE
   }
-  if (f.kind == kPreference && n > 0 && !f.adds_up) launch_kernel(k_loss_pairs, dim3(f.P), dim3(64), st, f, rows.T, ws);
+  const bool pairs = f.kind == kPreference;
+  if (pairs && n > 0 && !f.adds_up) launch_kernel(k_loss_pairs, dim3(f.P), dim3(64), st, f, rows.T, ws);
   if (grad && n > 0 && !(join && own_row)) {
-    const int per = max(kPiece, ((nv + kMostPieces - 1) / kMostPieces + 63) / 64 * 64), pieces = (nv + per - 1) / per;
+    // as many vectors per lane as leave each resident wavefront a piece, up to 8
+    const int64_t lanes = ((int64_t)n * nv + kResidentWaves - 1) / kResidentWaves;
+    const int fair = (int)min((int64_t)kPiece, (lanes + 63) / 64 * 64);
+    const int per = max(fair, ((nv + kMostPieces - 1) / kMostPieces + 63) / 64 * 64), pieces = (nv + per - 1) / per;
     const uint32_t groups = ((uint32_t)n * (uint32_t)pieces + kWaves - 1) / kWaves;
-    const dim3 grid(groups < kMostGroups ? groups : kMostGroups);
+    const dim3 grid((groups < kMostGroups ? groups : kMostGroups) + (pairs ? 1 : 0));
 #define ADASD_GRAD_CASE(DTV, REFV) \
     if (dt == DTV && by_ref == REFV) \
-      launch_kernel((k_loss_grad<DTV, REFV>), grid, block, st, rows, pieces, per, ws, f.kind == kPreference ? 1 : 0, ent ? 1 : 0);
+      launch_kernel((k_loss_grad<DTV, REFV>), grid, block, st, rows, pieces, per, ws, pairs ? f.P : 0, pairs ? f.loss : nullptr, ent ? 1 : 0);
     ADASD_GRAD_CASE(ADASD_BF16, false) ADASD_GRAD_CASE(ADASD_BF16, true) ADASD_GRAD_CASE(ADASD_F32, false) ADASD_GRAD_CASE(ADASD_F32, true)
 #undef ADASD_GRAD_CASE
   }
-  if (f.loss && !f.adds_up) {
-    const bool pairs = f.kind == kPreference;
+  if (f.loss && (pairs ? n == 0 || !grad : !f.adds_up)) {
     launch_kernel(k_loss_total, dim3(1), dim3(64), st, pairs ? ws.pair : ws.term, n == 0 ? 0 : pairs ? f.P : n, f.loss);
   }
   return hipGetLastError();

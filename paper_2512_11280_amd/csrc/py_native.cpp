@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/core/TensorImpl.h>
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
@@ -465,27 +466,54 @@ struct RowsCall {
   }
 };
 
-// Objects to be handed over together.
-template <int M> struct Objects {
+// Results to be handed over together: the caller's tensors, or parts of one allocation for all that are new (a tensor of its own takes
+// 0.7 us each, more than the smallest call has to spare; a part that is kept keeps the others' memory, 20 bytes a position).
+template <int M> struct Results {
+  const RowsCall& c;
   PyObject* o[M] = {};
+  int64_t elements[M], at[M], bytes = 0;
+  at::ScalarType type[M];
+  at::SmallVector<int64_t, 2> size[M];
   int n = 0;
-  ~Objects() {
+  explicit Results(const RowsCall& call) : c(call) {}
+  ~Results() {
     for (int i = 0; i < n; ++i) Py_XDECREF(o[i]);
   }
-  void add(PyObject* p) { o[n++] = p; }
-  template <class T> T* make(const RowsCall& c, at::IntArrayRef size, at::ScalarType type) {
-    at::Tensor t = at::empty(size, c.z->options().dtype(type));
-    T* p = (T*)t.data_ptr();
-    add(RowsCall::wrap(std::move(t)));
-    return p;
+  Results(const Results&) = delete;
+  int add(PyObject* p) {                       // an object as it is
+    o[n] = p;
+    return n++;
   }
-  template <class T> T* take(const RowsCall& c, PyObject* o, at::ScalarType type, const char* name) {     // the caller's, or a new one
-    if (!given(o)) return make<T>(c, at::IntArrayRef(c.shape, c.dims), type);
-    T* p = (T*)c.input(o, type, name);
-    Py_INCREF(o);
-    add(o);
-    return p;
+  int make(at::IntArrayRef sizes, at::ScalarType t) {
+    size[n].assign(sizes.begin(), sizes.end());
+    type[n] = t;
+    int64_t count = 1;
+    for (int64_t d : sizes) count *= d;
+    at[n] = bytes;
+    bytes += (4 * count + 63) / 64 * 64;       // (every result has elements of 4 bytes)
+    return n++;
   }
+  int take(PyObject* given_one, at::ScalarType t, const char* name) {      // the caller's, in the shape of the tokens, or a new one
+    if (!given(given_one)) return make(at::IntArrayRef(c.shape, c.dims), t);
+    c.input(given_one, t, name);
+    Py_INCREF(given_one);
+    return add(given_one);
+  }
+  void allocate() {
+    bool missing = false;
+    for (int i = 0; i < n; ++i) missing = missing || !o[i];
+    if (!missing) return;
+    const at::Tensor all = at::empty({bytes / 4}, c.z->options().dtype(at::kFloat));
+    for (int i = 0; i < n; ++i) {
+      if (o[i]) continue;
+      auto part = c10::make_intrusive<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(all.storage()), all.key_set(),
+                                                       c10::scalarTypeToTypeMeta(type[i]));
+      part->set_sizes_contiguous(size[i]);
+      part->set_storage_offset(at[i] / 4);
+      o[i] = RowsCall::wrap(at::Tensor(std::move(part)));
+    }
+  }
+  template <class T> T* ptr(int i) const { return (T*)THPVariable_Unpack(o[i]).data_ptr(); }
   PyObject* tuple() {
     PyObject* r = PyTuple_New(n);
     if (!r) throw Fail{};
@@ -493,8 +521,8 @@ template <int M> struct Objects {
     n = 0;
     return r;
   }
-  PyObject* call(PyObject* type) {
-    PyObject* r = PyObject_Vectorcall(type, o, n, nullptr);
+  PyObject* call(PyObject* result) {
+    PyObject* r = PyObject_Vectorcall(result, o, n, nullptr);
     if (!r) throw Fail{};
     return r;
   }
@@ -521,10 +549,14 @@ PyObject* py_token_logprob(PyObject*, PyObject* const* args, Py_ssize_t nargs, P
     parse("token_logprob", names, 3, args, nargs, kw, a);
     RowsCall c(a[0], a[1], a[2], false);
     c.rows.active = (const uint8_t*)c.maybe(a[3], at::kByte, "active");
-    Objects<3> out;
-    c.rows.logprob = out.take<float>(c, a[4], at::kFloat, "logprob_out");
-    c.rows.entropy = out.take<float>(c, a[5], at::kFloat, "entropy_out");
-    c.rows.status = out.take<uint32_t>(c, a[6], at::kInt, "status_out");
+    Results<3> out(c);
+    out.take(a[4], at::kFloat, "logprob_out");
+    out.take(a[5], at::kFloat, "entropy_out");
+    out.take(a[6], at::kInt, "status_out");
+    out.allocate();
+    c.rows.logprob = out.ptr<float>(0);
+    c.rows.entropy = out.ptr<float>(1);
+    c.rows.status = out.ptr<uint32_t>(2);
     enqueue("adasd_token_logprob", [&] { return g_abi.token_logprob(&c.rows, c.stream); });
     return out.tuple();
   });
@@ -540,7 +572,7 @@ PyObject* py_token_logprob_grad(PyObject*, PyObject* const* args, Py_ssize_t nar
     const float* dlp = (const float*)c.input(a[3], at::kFloat, "dlogprob");
     const float* dent = (const float*)c.maybe(a[4], at::kFloat, "dentropy");
     c.rows.active = (const uint8_t*)c.maybe(a[5], at::kByte, "active");
-    Objects<1> out;
+    Results<1> out(c);
     out.add(c.gradient(a[6]));
     enqueue("adasd_token_logprob_grad", [&] { return g_abi.token_logprob_grad(&c.rows, dlp, dent, c.stream); });
     out.n = 0;
@@ -579,16 +611,19 @@ PyObject* py_policy_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyO
       p.entropy_coef = float_attr(a[8], N->entropy_coef);
     }
     p.grad_scale = c.one(a[9], 1, "grad_scale");
-    Objects<7> out;
+    Results<7> out(c);
     const at::IntArrayRef size(c.shape, c.dims);
-    p.loss = out.make<float>(c, {}, at::kFloat);
-    p.token_loss = out.make<float>(c, size, at::kFloat);
-    c.rows.logprob = out.make<float>(c, size, at::kFloat);
-    c.rows.entropy = out.make<float>(c, size, at::kFloat);
-    p.kl = out.make<float>(c, size, at::kFloat);
-    c.rows.status = out.make<uint32_t>(c, size, at::kInt);
-    if (truth(a[10], true)) out.add(c.gradient(a[11]));
-    else out.add(Py_NewRef(Py_None));
+    out.make({}, at::kFloat);
+    for (int i = 1; i < 5; ++i) out.make(size, at::kFloat);
+    out.make(size, at::kInt);
+    out.allocate();
+    p.loss = out.ptr<float>(0);
+    p.token_loss = out.ptr<float>(1);
+    c.rows.logprob = out.ptr<float>(2);
+    c.rows.entropy = out.ptr<float>(3);
+    p.kl = out.ptr<float>(4);
+    c.rows.status = out.ptr<uint32_t>(5);
+    out.add(truth(a[10], true) ? c.gradient(a[11]) : Py_NewRef(Py_None));
     enqueue("adasd_policy_loss", [&] { return g_abi.policy_loss(&c.rows, &p, c.stream); });
     return out.call(g_policy_result);
   });
@@ -619,16 +654,20 @@ PyObject* py_preference_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs,
       p.label_smoothing = float_attr(a[6], N->label_smoothing);
     }
     p.grad_scale = c.one(a[7], 1, "grad_scale");
-    Objects<7> out;
-    const at::IntArrayRef size(c.shape, 2), pairs(&P, 1), sequences(c.shape, 1);
-    p.loss = out.make<float>(c, {}, at::kFloat);
-    p.pair_loss = out.make<float>(c, pairs, at::kFloat);
-    p.pair_margin = out.make<float>(c, pairs, at::kFloat);
-    p.score = out.make<float>(c, sequences, at::kFloat);
-    c.rows.logprob = out.make<float>(c, size, at::kFloat);
-    c.rows.status = out.make<uint32_t>(c, size, at::kInt);
-    if (truth(a[8], true)) out.add(c.gradient(a[9]));
-    else out.add(Py_NewRef(Py_None));
+    Results<7> out(c);
+    out.make({}, at::kFloat);
+    for (int i = 1; i < 3; ++i) out.make(at::IntArrayRef(&P, 1), at::kFloat);
+    out.make(at::IntArrayRef(c.shape, 1), at::kFloat);
+    out.make(at::IntArrayRef(c.shape, 2), at::kFloat);
+    out.make(at::IntArrayRef(c.shape, 2), at::kInt);
+    out.allocate();
+    p.loss = out.ptr<float>(0);
+    p.pair_loss = out.ptr<float>(1);
+    p.pair_margin = out.ptr<float>(2);
+    p.score = out.ptr<float>(3);
+    c.rows.logprob = out.ptr<float>(4);
+    c.rows.status = out.ptr<uint32_t>(5);
+    out.add(truth(a[8], true) ? c.gradient(a[9]) : Py_NewRef(Py_None));
     enqueue("adasd_preference_loss", [&] { return g_abi.preference_loss(&c.rows, &p, c.stream); });
     return out.call(g_preference_result);
   });
