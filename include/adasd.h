@@ -376,8 +376,8 @@ int adasd_update_thresholds(const adasd_state *st /* host */, int k_max, const i
  * All calls below describe their rows by an adasd_rows: B sequences of T positions with one token each.
  *   position (b,t) : p = softmax(logits[b,t,:]), x = tokens[b,t];
  *   logprob[b,t]   = ln p(x);   entropy[b,t] = H(p) in nats (Appendix A of the paper);
- *   a position with weight[b,t] == 0 (or active[b,t] == 0) does not count: its logits, token and other inputs are not read (they
- *   need not be numbers), its results are 0, and its row of dlogits is written with zeros;
+ *   a position with weight[b,t] == 0 (or active[b,t] == 0) does not count: its logits, token and other inputs enter no result (they
+ *   need not be numbers, or a token of the vocabulary), its results are 0, and its row of dlogits is written with zeros;
  *   status[b,t]    = ADASD_ST_BAD_TOKEN (token outside [0,V): log-probability NaN), ADASD_ST_NONFINITE (NaN/+inf in the row, or no
  *                    logit above -2^120: results NaN), or 0.  A gradient row that depends on a NaN is NaN.
  * Logits of -inf, or of the type's lowest value beside ordinary ones, are tokens without mass: gradient 0 there.

@@ -273,19 +273,12 @@ template <int DT, bool REF> __device__ __noinline__ LossSums wave_sums(const cha
 
 // A slice's vectors come in batches of four per thread, the next batch on its way.
 constexpr int kSumsBatch = 4;
-template <int DT, bool REF, bool PAST> __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f, int S, int chunk, LossWorkspace ws) {
+template <int DT, bool REF, bool PAST> __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f, int S, int chunk, int early, LossWorkspace ws) {
+  warm_kernargs<sizeof(LossRows) + sizeof(LossTerm) + 4 * sizeof(int) + sizeof(LossWorkspace)>();
   __shared__ LossSums sh[kWaves];
   const int r = blockIdx.x / S, s = blockIdx.x - r * S, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = r / rows.T, t = r - b * rows.T, V = rows.V;
-  if (!position_counts(rows, r)) {
-    if (s != 0 || wave != 0) return;
-    if (lane == 0) {
-      report_nothing(rows, f, r);
-      ws.coef[r] = LossCoef{};
-    }
-    position_done(rows, f, ws, r, 0.0);
-    return;
-  }
+  const PositionMark mark = ask_mark(rows, r);
   PositionIn in = ask_position(rows, f, r, b);
   const char* row = row_at<DT>(rows.z, b, t);
   const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
@@ -296,12 +289,25 @@ template <int DT, bool REF, bool PAST> __global__ void __launch_bounds__(kBlock)
     return idx < whole ? load_whole<PAST>(from, idx) : load_last_vec<DT>(from, V);
   };
   uint4 next[kSumsBatch], nextr[kSumsBatch];
+  auto first_batch = [&] {
 #pragma unroll
-  for (int k = 0; k < kSumsBatch; ++k) next[k] = load(row, v0 + tid + k * kBlock);
-  if (REF) {
+    for (int k = 0; k < kSumsBatch; ++k) next[k] = load(row, v0 + tid + k * kBlock);
+    if (REF) {
 #pragma unroll
-    for (int k = 0; k < kSumsBatch; ++k) nextr[k] = load(ref, v0 + tid + k * kBlock);
+      for (int k = 0; k < kSumsBatch; ++k) nextr[k] = load(ref, v0 + tid + k * kBlock);
+    }
+  };
+  if (early) first_batch();
+  if (!position_counts(mark)) {
+    if (s != 0 || wave != 0) return;
+    if (lane == 0) {
+      report_nothing(rows, f, r);
+      ws.coef[r] = LossCoef{};
+    }
+    position_done(rows, f, ws, r, 0.0);
+    return;
   }
+  if (!early) first_batch();
   ask_logit<DT>(in, row, V);
   const float c = REF ? ref_shift<DT>(row, ref, in.x, V) : 0.f;
   LossSums a = loss_empty();
@@ -445,6 +451,7 @@ constexpr uint32_t kMostGroups = 1u << 22;
 constexpr int kResidentWaves = 8 * 4 * 256;
 template <int DT, bool REF>
 __global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces, int per, LossWorkspace ws, int P, float* loss, int ent) {
+  warm_kernargs<sizeof(LossRows) + 4 * sizeof(int) + sizeof(LossWorkspace) + sizeof(float*)>();
   const int lane = threadIdx.x & 63, V = rows.V, nv = vectors_of<DT>(V);
   const uint32_t step = (gridDim.x - (loss ? 1u : 0u)) * kWaves, units = (uint32_t)rows.n * (uint32_t)pieces;
   if (loss && blockIdx.x == gridDim.x - 1) {         // (the pairs' sum; its workgroup is one more than the rows take)
@@ -536,7 +543,8 @@ __device__ __forceinline__ uint64_t send_results(uint64_t* at, int S, int own, c
 // Wavefronts per SIMD that the registers are limited for (64 of data and about 50 more: four; 16: eight).
 constexpr int join_waves(int nb, bool ref) { return !ref ? (nb <= 4 ? 8 : nb <= 8 ? 6 : 4) : (nb <= 2 ? 7 : nb <= 4 ? 5 : 4); }
 template <int DT, bool REF, int NB, int WPR, bool PAST>
-__global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(NB, REF)) k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, LossWorkspace ws) {
+__global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(NB, REF)) k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, LossWorkspace ws) {
+  warm_kernargs<sizeof(LossRows) + sizeof(LossTerm) + 4 * sizeof(int) + sizeof(LossWorkspace)>();
   constexpr int RPB = WPR < kWaves ? kWaves / WPR : 1, TR = 64 * WPR;          // rows per workgroup, threads per row
   __shared__ JoinShared<WPR < kWaves ? kWaves : WPR> sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), V = rows.V, nv = vectors_of<DT>(V);
@@ -544,22 +552,22 @@ __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(N
   const int sub = wave / WPR, r = r0 + sub, me = tid & (TR - 1);
   const bool here = r < rows.n;
   const int b = here ? r / rows.T : 0, t = here ? r - b * rows.T : 0;
-  const bool on = here && position_counts(rows, r);
+  const int r_here = here ? r : 0;
+  const PositionMark mark = ask_mark(rows, r_here);
+  int x = rows.tokens[r_here];
   const char* row = row_at<DT>(rows.z, b, t);
   const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
   const int v0 = min(s * chunk, nv), v1 = min(v0 + chunk, nv);
   // what the positions are settled from, a pair of lanes for each row of the workgroup
   const int i = RPB > 1 ? min(lane >> 1, RPB - 1) : 0, ri = min(r0 + i, rows.n - 1), bi = ri / rows.T;
   PositionIn in{};
-  bool on_i = on;
-  if (wave == 0) {
-    if (RPB > 1) on_i = r0 + i < rows.n && position_counts(rows, ri);
-    if (on_i && s == S - 1) in = ask_position(rows, f, ri, bi);
+  PositionMark mark_i = mark;
+  if (wave == 0 && s == S - 1) {
+    in = ask_position(rows, f, ri, bi);
+    if (RPB > 1) mark_i = ask_mark(rows, ri);
   }
   uint4 v[NB], q[NB];
-  int x = -1;
-  if (here) x = rows.tokens[r];
-  if (on) {
+  auto load_row = [&] {
     const int full = min(v1, V / Elem<DT>::per_vec);
     auto load = [&](const char* from, int j) {
       const int idx = v0 + me + j * TR;
@@ -572,9 +580,11 @@ __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(N
 #pragma unroll
       for (int j = 0; j < NB; ++j) q[j] = load(ref, j);
     }
-  }
-  const char* row_i = row_at<DT>(rows.z, bi, ri - bi * rows.T);
-  if (wave == 0 && on_i && s == S - 1) ask_logit<DT>(in, row_i, V);
+  };
+  if (early) load_row();
+  const bool on = here && position_counts(mark), on_i = RPB > 1 ? r0 + i < rows.n && position_counts(mark_i) : on;
+  if (on && !early) load_row();
+  if (wave == 0 && on_i && s == S - 1) ask_logit<DT>(in, row_at<DT>(rows.z, bi, ri - bi * rows.T), V);
   float c = 0.f;
   if (on) {
     if (REF) c = ref_shift<DT>(row, ref, x, V);
@@ -654,6 +664,8 @@ __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(N
   if (!here || (RPB == 1 && sh.role == kLeaves)) return;
   char* out = rows.g.base ? const_cast<char*>(row_at<DT>(rows.g, b, t)) : nullptr;
   const LossCoef k = sh.coef[sub];
+  // (beside the other wavefronts' part of the gradient)
+  if (RPB == 1 && wave == 0 && (sh.role == kSettles || (!on && s == 0))) position_done(rows, f, ws, r, term);
   if (out) {
     if (zero_row(k)) {
       for (int idx = v0 + me; idx < v1; idx += TR) zero_vec<DT>(out, idx, V);
@@ -665,12 +677,7 @@ __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(N
       }
     }
   }
-  if (RPB > 1) return;
-  if (S == 1 || !on) {
-    if (wave == 0 && s == 0) position_done(rows, f, ws, r, term);
-    return;
-  }
-  if (sh.role != kSettles) return;
+  if (RPB > 1 || S == 1 || !on || sh.role != kSettles) return;
   // ---- the slices that have ended without their results
   if (wave == 0) {
     uint64_t left = __ballot(found == kLeft);
@@ -690,7 +697,6 @@ __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(N
       emit_vec<DT, REF>(out, idx, V, x, z, REF ? load_vec_of<DT>(ref, idx, V) : z, k, ent);
     }
   }
-  if (wave == 0) position_done(rows, f, ws, r, term);
 }
 
 }  // namespace
@@ -733,6 +739,8 @@ JoinPlan join_plan(int n, int nv, bool ref) {
 // Logits of so many bytes are read past the caches.  Gradients of one launch read them once (1024 rows of 152064 bf16 and a reference's 226 -> 218
 // us, 200000 rows of 2000 493 -> 453; 385 rows of 32003 float and a reference's, which the cache behind the L2s can hold from the kernel
 // that wrote them, 34 -> 35).  Log-probabilities are often asked for ahead of a gradient, so only what that cache cannot hold.
+// Of so few bytes the logits are asked for before it is known whether their position counts: one latency less.
+constexpr int64_t kEarly = (int64_t)16 << 20;
 constexpr int64_t kJoinPast = (int64_t)64 << 20, kSumsPast = (int64_t)256 << 20;
 
 hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorkspace& ws, hipStream_t st) {
@@ -744,6 +752,7 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
   const JoinPlan plan = join_plan(n, nv, ref);
   const bool join = n > 0 && plan.S > 0 && (plan.S == 1 || (int64_t)plan.S * n <= ws.slices) && (own_row || plan.wpr < 4);
   const int64_t bytes = (int64_t)n * nv * 16;
+  const bool early = bytes <= kEarly;
   const bool past = join ? own_row && bytes > kJoinPast : f.kind == kLogprob && bytes > kSumsPast;
   f.adds_up = f.loss && n > 0 && (join ? plan.wpr >= kWaves && n <= kJoinAddsUp : n <= kAddsUp);
   if (join) {
@@ -753,7 +762,7 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
 #define ADASD_JOIN_CASE(DTV, REFV, NBV, WPRV, PASTV) \
     if (dt == DTV && ref == REFV && plan.nb == NBV && plan.wpr == WPRV && past == PASTV) \
       launch_kernel((k_loss_join<DTV, REFV, NBV, WPRV, PASTV>), dim3(groups), dim3(WPRV > kWaves ? 64 * WPRV : kBlock), st, some, f, plan.S, \
-                    plan.chunk, ent ? 1 : 0, ws);
+                    plan.chunk, ent ? 1 : 0, early ? 1 : 0, ws);
 #define ADASD_JOIN_CASES(REFV, NBV, WPRV) \
     ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, false) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, false) \
     ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, true) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, true)
@@ -767,7 +776,7 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
     const int S = scan_split(n, rows.V, dt), chunk = slice_chunk(nv, S);
 #define ADASD_LOSS_CASE(DTV, REFV, PASTV) \
     if (dt == DTV && ref == REFV && past == PASTV) \
-      launch_kernel((k_loss_sums<DTV, REFV, PASTV>), dim3(n * S), block, st, rows, f, S, chunk, ws);
+      launch_kernel((k_loss_sums<DTV, REFV, PASTV>), dim3(n * S), block, st, rows, f, S, chunk, early ? 1 : 0, ws);
     ADASD_LOSS_CASE(ADASD_BF16, false, false) ADASD_LOSS_CASE(ADASD_BF16, true, false) ADASD_LOSS_CASE(ADASD_F32, false, false)
     ADASD_LOSS_CASE(ADASD_F32, true, false) ADASD_LOSS_CASE(ADASD_BF16, false, true) ADASD_LOSS_CASE(ADASD_F32, false, true)
 #undef ADASD_LOSS_CASE

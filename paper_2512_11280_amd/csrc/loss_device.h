@@ -158,10 +158,15 @@ template <bool REF> __device__ __forceinline__ LossRow finish_loss_row(const Los
   return r;
 }
 
-__device__ __forceinline__ bool position_counts(const LossRows& rows, int r) {
-  if (rows.weight) return rows.weight[r] != 0.f;
-  return rows.active ? rows.active[r] != 0 : true;
+// Whether a position counts, in two steps: what says so is asked for, and looked at where it is needed.
+struct PositionMark {
+  float weight;
+  uint8_t active;
+};
+__device__ __forceinline__ PositionMark ask_mark(const LossRows& rows, int r) {
+  return PositionMark{rows.weight ? rows.weight[r] : 1.f, rows.active ? rows.active[r] : (uint8_t)1};
 }
+__device__ __forceinline__ bool position_counts(const PositionMark& m) { return m.weight != 0.f && m.active != 0; }
 template <int DT> __device__ __forceinline__ const char* row_at(const RowPlace& p, int b, int t) {
   return static_cast<const char*>(p.base) + ((int64_t)b * p.seq + (int64_t)t * p.pos) * Elem<DT>::bytes;
 }
