@@ -236,7 +236,6 @@ constexpr int kTicketLossLen = 32768;
 // Up to so many positions the last one done adds up the loss, which saves a launch or two (3 to 5 us); of more, that many additions to one
 // counter come one after the other, and a launch of its own is lost beside what they take.
 constexpr int kAddsUp = 4096, kJoinAddsUp = 256;
-constexpr int kJoinResident = 4 * 256;                   // workgroups of k_loss_join that the chip holds
 size_t loss_workspace_bytes_for(int64_t positions, int V, int dt);
 size_t loss_workspace_layout(size_t ws_bytes, LossWorkspace* ws, void* base);
 hipError_t launch_loss(const LossRows& rows, int dt, LossTerm term, const LossWorkspace& ws, hipStream_t st);

@@ -449,7 +449,7 @@ __device__ __forceinline__ void emit_vec(char* out, int idx, int V, int x, const
 constexpr int kPiece = 8 * 64, kMostPieces = 2048;      // (2^20 rows: no more than 2^31 pieces)
 constexpr uint32_t kMostGroups = 1u << 22;
 constexpr int kResidentWaves = 8 * 4 * 256;
-template <int DT, bool REF>
+template <int DT, bool REF, bool PAST>
 __global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces, int per, LossWorkspace ws, int P, float* loss, int ent) {
   warm_kernargs<sizeof(LossRows) + 4 * sizeof(int) + sizeof(LossWorkspace) + sizeof(float*)>();
   const int lane = threadIdx.x & 63, V = rows.V, nv = vectors_of<DT>(V);
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces,
     }
     const int x = rows.tokens[r];
     for (int idx = v0 + lane; idx < v1; idx += 64) {
-      const uint4 z = load_vec_of<DT>(row, idx, V);
+      const uint4 z = idx < V / Elem<DT>::per_vec ? load_whole<PAST>(row, idx) : load_last_vec<DT>(row, V);
       emit_vec<DT, REF>(out, idx, V, x, z, REF ? load_vec_of<DT>(ref, idx, V) : z, k, ent);
     }
   }
@@ -704,7 +704,10 @@ __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(N
 namespace {
 
 // How k_loss_join cuts rows of nv vectors: wavefronts per row, vectors in registers per thread, slices (0: too long) and vectors per slice.
-//  * Few rows: as many slices of a workgroup of four wavefronts as are resident together.
+//  * Few rows: as many slices as are resident together, of eight wavefronts and up to 8 vectors per thread (with a reference's row four
+//    wavefronts and up to 4 + 4); where those would not all be, and would be with twice the vectors, that.  (Us a call, eight wavefronts x 8 / four x
+//    16: 64 rows of 32000 bf16 9.4 / 11.8, 512 19.4 / 21.2, 256 of 32003 float 18.6 / 20.9, 256 of 128256 bf16 30.7 / 28.1.  With a
+//    reference, 4 + 4 / 8 + 8: 64 of 32000 12.4 / 15.4, 128 14.5 / 16.6, but 256 of 128256 63 / 59.)
 //  * Many short rows: as few wavefronts per row as hold it, with as few registers as it takes (rows of 2000 bf16, four wavefronts
 //    each / one / one of few registers: 200000 rows 1463 / 703 / 536 us; of 8000, four / two / one: 50000 rows 529 / 369 / 364).
 //  * Many long rows: eight wavefronts of 8 vectors per thread, three workgroups per compute unit.  Bytes on their way are what the
@@ -717,28 +720,31 @@ struct JoinPlan {
   int wpr, nb, S, chunk;
 };
 JoinPlan join_plan(int n, int nv, bool ref) {
-  const int most = ref ? 8 : 16;
-  if (n > kJoinResident) {
-    for (int nb = most / 4; nb <= most; nb *= 2)
-      if (nv <= 64 * nb) return {1, nb, 1, nv};
-    if (nv <= 128 * most) return {2, most, 1, nv};
-    if (ref && nv <= 256 * most) return {4, most, 1, nv};
-    if (nv <= 512 * 8) return {8, 8, 1, nv};
-    const int wpr = ref ? 4 : 8, S = (nv + 512 * wpr - 1) / (512 * wpr);
-    return {wpr, 8, S <= kMaxSplit ? S : 0, slice_chunk(nv, S)};
+  const int most = ref ? 8 : 16, wpr_few = ref ? 4 : 8, nb_few = ref ? 4 : 8;
+  const int64_t resident = ref ? 5 * 256 : 3 * 256;
+  for (int turns = 1; turns <= nb_few; ++turns) {
+    const int lanes = 64 * wpr_few * turns, S = (nv + lanes - 1) / lanes;
+    if (S <= kMaxSplit && (int64_t)S * n <= resident) return {wpr_few, nb_few, S, slice_chunk(nv, S)};
   }
-  for (int turns = 1; turns <= most; ++turns) {
+  for (int turns = nb_few + 1; turns <= most; ++turns) {
     const int S = (nv + turns * kBlock - 1) / (turns * kBlock);
-    if (S <= kMaxSplit && (turns == most || (int64_t)S * n <= kJoinResident)) return {4, most, S, slice_chunk(nv, S)};
+    if (S <= kMaxSplit && (int64_t)S * n <= 4 * 256) return {4, most, S, slice_chunk(nv, S)};
   }
-  return {4, most, 0, 0};
+  for (int nb = most / 4; nb <= most; nb *= 2)
+    if (nv <= 64 * nb) return {1, nb, 1, nv};
+  if (nv <= 128 * most) return {2, most, 1, nv};
+  if (ref && nv <= 256 * most) return {4, most, 1, nv};
+  if (nv <= 512 * 8) return {8, 8, 1, nv};
+  const int wpr = ref ? 4 : 8, S = (nv + 512 * wpr - 1) / (512 * wpr);
+  return {wpr, 8, S <= kMaxSplit ? S : 0, slice_chunk(nv, S)};
 }
 
 }  // namespace
 
 // Logits of so many bytes are read past the caches.  Gradients of one launch read them once (1024 rows of 152064 bf16 and a reference's 226 -> 218
 // us, 200000 rows of 2000 493 -> 453; 385 rows of 32003 float and a reference's, which the cache behind the L2s can hold from the kernel
-// that wrote them, 34 -> 35).  Log-probabilities are often asked for ahead of a gradient, so only what that cache cannot hold.
+// that wrote them, 34 -> 35).  Log-probabilities are often asked for ahead of a gradient, so only what that cache cannot hold;
+// the second read of a preference loss likewise (200000 rows of 2000 bf16 500 -> 447 us, 256 of 128256 44 -> 45).
 // Of so few bytes the logits are asked for before it is known whether their position counts: one latency less.
 constexpr int64_t kEarly = (int64_t)16 << 20;
 constexpr int64_t kJoinPast = (int64_t)64 << 20, kSumsPast = (int64_t)256 << 20;
@@ -769,7 +775,7 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
     ADASD_JOIN_CASES(false, 4, 1) ADASD_JOIN_CASES(false, 8, 1) ADASD_JOIN_CASES(false, 16, 1) ADASD_JOIN_CASES(false, 16, 2)
     ADASD_JOIN_CASES(false, 16, 4) ADASD_JOIN_CASES(false, 8, 8)
     ADASD_JOIN_CASES(true, 2, 1) ADASD_JOIN_CASES(true, 4, 1) ADASD_JOIN_CASES(true, 8, 1) ADASD_JOIN_CASES(true, 8, 2)
-    ADASD_JOIN_CASES(true, 8, 4) ADASD_JOIN_CASES(true, 8, 8)
+    ADASD_JOIN_CASES(true, 8, 4) ADASD_JOIN_CASES(true, 8, 8) ADASD_JOIN_CASES(true, 4, 4)
 #undef ADASD_JOIN_CASES
 #undef ADASD_JOIN_CASE
   } else if (n > 0) {
@@ -789,11 +795,15 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
     const int fair = (int)min((int64_t)kPiece, (lanes + 63) / 64 * 64);
     const int per = max(fair, ((nv + kMostPieces - 1) / kMostPieces + 63) / 64 * 64), pieces = (nv + per - 1) / per;
     const uint32_t groups = ((uint32_t)n * (uint32_t)pieces + kWaves - 1) / kWaves;
+    const bool last_past = bytes > kSumsPast;
     const dim3 grid((groups < kMostGroups ? groups : kMostGroups) + (pairs ? 1 : 0));
-#define ADASD_GRAD_CASE(DTV, REFV) \
-    if (dt == DTV && by_ref == REFV) \
-      launch_kernel((k_loss_grad<DTV, REFV>), grid, block, st, rows, pieces, per, ws, pairs ? f.P : 0, pairs ? f.loss : nullptr, ent ? 1 : 0);
-    ADASD_GRAD_CASE(ADASD_BF16, false) ADASD_GRAD_CASE(ADASD_BF16, true) ADASD_GRAD_CASE(ADASD_F32, false) ADASD_GRAD_CASE(ADASD_F32, true)
+#define ADASD_GRAD_CASE(DTV, REFV, PASTV) \
+    if (dt == DTV && by_ref == REFV && last_past == PASTV) \
+      launch_kernel((k_loss_grad<DTV, REFV, PASTV>), grid, block, st, rows, pieces, per, ws, pairs ? f.P : 0, pairs ? f.loss : nullptr, \
+                    ent ? 1 : 0);
+    ADASD_GRAD_CASE(ADASD_BF16, false, false) ADASD_GRAD_CASE(ADASD_BF16, true, false) ADASD_GRAD_CASE(ADASD_F32, false, false)
+    ADASD_GRAD_CASE(ADASD_F32, true, false) ADASD_GRAD_CASE(ADASD_BF16, false, true) ADASD_GRAD_CASE(ADASD_BF16, true, true)
+    ADASD_GRAD_CASE(ADASD_F32, false, true) ADASD_GRAD_CASE(ADASD_F32, true, true)
 #undef ADASD_GRAD_CASE
   }
   if (f.loss && (pairs ? n == 0 || !grad : !f.adds_up)) {
