@@ -378,11 +378,12 @@ int adasd_update_thresholds(const adasd_state *st /* host */, int k_max, const i
  *   logprob[b,t]   = ln p(x);   entropy[b,t] = H(p) in nats (Appendix A of the paper);
  *   a position with weight[b,t] == 0 (or active[b,t] == 0) does not count: its logits, token and other inputs enter no result (they
  *   need not be numbers, or a token of the vocabulary), its results are 0, and its row of dlogits is written with zeros;
- *   status[b,t]    = ADASD_ST_BAD_TOKEN (token outside [0,V): log-probability NaN), ADASD_ST_NONFINITE (NaN/+inf in the row, or no
- *                    logit above -2^120: results NaN), or 0.  A gradient row that depends on a NaN is NaN.
+ *   status[b,t]    = ADASD_ST_BAD_TOKEN (token outside [0,V): log-probability NaN), ADASD_ST_NONFINITE (NaN, +inf or a logit of
+ *                    2^120 or more in the row, or none above -2^120: results NaN), or 0.  A gradient row that depends on a NaN
+ *                    is NaN.
  * Logits of -inf, or of the type's lowest value beside ordinary ones, are tokens without mass: gradient 0 there.
  * Gradients have the type of the logits (formed in 32 bits, rounded once).  dlogits may be the logits' own memory (same pointer and
- * strides: the gradient takes their place); any other overlap with logits the call reads is refused.
+ * strides: the gradient takes their place); any other address range that overlaps that of logits the call reads is refused.
  * Strides as everywhere here are in elements; rows may lie in either order (a [T,B,V] array seen as [B,T,V] is fine, and so is a
  * view that leaves out positions) but must not overlap.  B*T <= ADASD_MAX_ROWS.  No call synchronises, allocates or keeps anything
  * from one call for the next; sums are taken in a fixed order, so results are reproducible bit for bit.
@@ -407,8 +408,8 @@ typedef struct {
   size_t ws_bytes;
 } adasd_rows;
 
-/* Scratch of the calls below for B x T positions over V (serves any smaller B*T, and any V up to this one).  Calls that share
- * one must be ordered on one stream. */
+/* Scratch of the calls below for B x T positions over V (serves any smaller B*T; with a longer V, or logits of another type, the
+ * same results may take longer).  Calls that share one must be ordered on one stream. */
 int adasd_loss_workspace_bytes(int B, int T, int V, adasd_dtype dt, size_t *bytes /* host */);
 
 /* logprob, entropy and status of every active position (dlogits is not touched).  One read of the logits. */

@@ -551,3 +551,100 @@ def test_slices_whose_records_are_not_waited_for(am, how, dtype):
                 R.near(out, *R.grad(o, a, h, dtype=dtype), "dlogits")
             rows.logits = z.data_ptr()
             assert torch.equal(am.token_logprob_grad(z, x, ws, a.cuda(), h.cuda()), am.token_logprob_grad(z, x, c.ws(am), a.cuda(), h.cuda()))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("layout", ["view", "in_place", "offset"])
+def test_layouts_of_many_rows(am, layout, dtype):
+    B, T, V = 31, 43, 1037
+    c = Case(B, T, V, dtype, seed=26)
+    if layout == "view":
+        z, g = (torch.full((B, T + 1, V), 7.0, dtype=dtype, device="cuda")[:, :T] for _ in range(2))
+    elif layout == "in_place":
+        z = torch.full((T, B, V + 3), 7.0, dtype=dtype, device="cuda")[..., :V].transpose(0, 1)
+        g = z
+    else:
+        z, g = (torch.full((B * T * V + 8,), 7.0, dtype=dtype, device="cuda")[k:k + B * T * V].view(B, T, V) for k in (1, 3))
+    z.copy_(c.z)
+    adv, old = c.n(B, T), c.old()
+    o = am.policy_loss(z, c.x.cuda(), adv.cuda(), c.ws(am), weight=c.w.cuda(), old_logprob=old.cuda(), options=am.PolicyOptions(entropy_coef=0.01), dlogits=g)
+    e = R.policy(c.z, c.x, adv, weight=c.w, old=old, ent=0.01)
+    R.near(o.loss, e["loss"], e["loss_tol"], "loss")
+    R.near(g, e["g"], e["g_tol"], "dlogits")
+    total = g._base if g._base is not None else g
+    inside = torch.zeros_like(total, dtype=torch.bool)
+    inside.as_strided(g.shape, g.stride(), g.storage_offset()).fill_(True)
+    assert (total[~inside] == 7.0).all()
+
+
+def test_forms_without_gradient_or_coefficient(am):
+    """No gradient wanted, or a reference whose KL is only reported, in every cut of the rows."""
+    for B, T, V in ((2, 3, 40), (3, 5, 9001), (31, 43, 1037), (27, 48, 4009), (2, 600, 20011)):
+        c = Case(B, T, V, BF, seed=27)
+        _policy(am, c, "full", 0.1, need_grad=False)
+        _policy(am, c, "full", 0.1, kl_coef=0.0)
+        _policy(am, c, "none", need_grad=False)
+        c = Case(B + B % 2, T, V, BF, seed=28)
+        _preference(am, c, need_grad=False)
+
+
+def test_workspace_of_a_shorter_vocabulary(am):
+    """A workspace with less room for the slices' words than these rows take: the same results by another way."""
+    c = Case(3, 400, 40009, BF, seed=29)
+    small = am.LossWorkspace(3, 400, 50, BF)
+    _policy(am, c, "full", 0.01, ws=small)
+    c = Case(4, 300, 40009, BF, seed=30)
+    _preference(am, c, ws=small)
+
+
+def test_two_calls_at_once(am):
+    """Two streams, each with its workspace and slices that wait for one another, over and over; each call against its result alone."""
+    def make(shape, seed):
+        c = Case(*shape, BF, seed=seed)
+        d = dict(z=c.z.cuda(), x=c.x.cuda(), adv=c.n(c.B, c.T).cuda(), w=c.w.cuda(), ws=c.ws(am), zref=c.z.cuda().roll(1, 0))
+        return d
+
+    def call(d):
+        o = am.policy_loss(d["z"], d["x"], d["adv"], d["ws"], weight=d["w"], ref_logits=d["zref"], options=am.PolicyOptions(kl_coef=0.1))
+        p = am.preference_loss(d["z"], d["x"], d["ws"], weight=d["w"])
+        return [o.loss, o.kl, o.dlogits, p.loss, p.dlogits]
+    jobs = [make((2, 20, 70001), 31), make((4, 9, 128256), 32)]
+    want = [[t.clone() for t in call(d)] for d in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    got = [[], []]
+    for _ in range(20):
+        for k, (s, d) in enumerate(zip(streams, jobs)):
+            with torch.cuda.stream(s):
+                got[k].append(call(d))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for r in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(want[k], r))
+
+
+def test_two_graphs_on_one_workspace(am):
+    c, e = Case(2, 10, 70001, BF, seed=33), Case(3, 200, 2003, F, seed=34)
+    ws = am.LossWorkspace(3, 200, 70001, F)
+
+    def step(c):
+        z, x, adv, w = c.z.cuda(), c.x.cuda(), torch.ones(c.B, c.T, device="cuda"), c.w.cuda()
+        torch.cuda.synchronize()
+
+        def run():
+            o = am.policy_loss(z, x, adv, ws, weight=w, options=am.PolicyOptions(entropy_coef=0.01))
+            lp, H, _ = am.token_logprob(z, x, ws)
+            return [o.loss, o.token_loss, o.dlogits, lp, H]
+        want = [t.clone() for t in run()]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = run()
+        return graph, out, want, run           # (run keeps the inputs that the graph reads)
+    steps = [step(c), step(e)]
+    for k in range(6):
+        graph, out, want, _ = steps[k % 2]
+        for t in out:
+            t.fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), k
