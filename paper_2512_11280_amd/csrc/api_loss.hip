@@ -7,9 +7,9 @@ namespace adasd {
 
 namespace {
 constexpr size_t kSliceBytes = (kXchgWords + kResultWords) * sizeof(uint64_t);
-constexpr size_t kPerPosition = sizeof(LossCoef) + 2 * sizeof(double) + sizeof(float) + 2 * sizeof(int32_t) + kSlicesPerPosition * kSliceBytes;
-constexpr size_t kLossFixed = (size_t)kMaxLossSlices * kSliceBytes + (kTicketLossLen + 32 + kAddsUp) * sizeof(int32_t) +
-                              kAddsUp * sizeof(double) + 9 * 256;
+constexpr size_t kPerPosition = sizeof(LossCoef) + 2 * sizeof(double) + sizeof(float) + sizeof(uint64_t) + kSlicesPerPosition * kSliceBytes;
+constexpr size_t kLossFixed = (size_t)kMaxLossSlices * kSliceBytes + (32 + kAddsUp) * sizeof(int32_t) +
+                              kAddsUp * sizeof(double) + 8 * 256;
 }  // namespace
 
 // Room for the positions' arrays, and for the hand-off words of their slices at their longest (k_loss_join with a reference: 2048 vectors a
@@ -33,8 +33,7 @@ size_t loss_workspace_layout(size_t ws_bytes, LossWorkspace* ws, void* base) {
     return at;
   };
   ws->slices = kMaxLossSlices + (int64_t)cap * kSlicesPerPosition;
-  ws->ticket = reinterpret_cast<int32_t*>(take(kTicketLossLen * sizeof(int32_t)));
-  ws->sets = reinterpret_cast<int32_t*>(take(2 * cap * sizeof(int32_t)));
+  ws->sets = reinterpret_cast<uint64_t*>(take(cap * sizeof(uint64_t)));
   ws->done = reinterpret_cast<int32_t*>(take((32 + kAddsUp) * sizeof(int32_t)));
   ws->fresh = reinterpret_cast<double*>(take(kAddsUp * sizeof(double)));
   ws->xchg = reinterpret_cast<uint64_t*>(take((size_t)ws->slices * kSliceBytes));

@@ -218,8 +218,7 @@ struct LossCoef {       // of a position: its gradient row is a 1[j = x] + 2^(x_
   float m, a, k0, k1, k2, c, pad[2];
 };
 struct LossWorkspace {
-  int32_t* ticket;      // [kTicketLossLen] arrival words of the rows that k_loss_sums cuts into slices (see Arrivals), zero between launches
-  int32_t* sets;        // [positions][2] the same of k_loss_join
+  uint64_t* sets;       // [positions] arrival words of the rows cut into slices (records.h), zero between launches
   int32_t* done;        // [32 + kAddsUp] positions (or pairs) that are done, and positions of each pair; zero between launches
   double* fresh;        // [kAddsUp] terms of positions that the last one done adds up; zero between launches
   uint64_t* xchg;       // [slices][kXchgWords + kResultWords] hand-off words, zero between launches
@@ -230,9 +229,8 @@ struct LossWorkspace {
   int64_t slices;
 };
 constexpr int kResultWords = 4;                          // 64-bit words of the numbers of a gradient row, sent to a slice
-constexpr int kMaxLossSlices = 8 * kResidentGroups;      // of all rows that are cut into more than one (scan_split)
+constexpr int kMaxLossSlices = 8 * kResidentGroups;      // of all rows that k_loss_sums cuts into more than one (scan_split)
 constexpr int kSlicesPerPosition = 4;                    // hand-off words of so many more come with each position of a workspace
-constexpr int kTicketLossLen = 32768;
 // Up to so many positions the last one done adds up the loss, which saves a launch or two (3 to 5 us); of more, that many additions to one
 // counter come one after the other, and a launch of its own is lost beside what they take.
 constexpr int kAddsUp = 4096, kJoinAddsUp = 256;

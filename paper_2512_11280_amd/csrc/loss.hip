@@ -135,11 +135,51 @@ __device__ __forceinline__ void report_nothing(const LossRows& rows, const LossT
   if (f.kl) f.kl[r] = 0.f;
 }
 
-// ---- sums over positions, by one wavefront.  Where the terms come from other workgroups of the same launch (FRESH) they are 64-bit words that
-// say themselves that they are there (the lowest bit of the fraction is set; a cleared word is 0), and are cleared as they are read.  The
-// order of the additions is the same either way.
+// ---- sums over positions, of M arrays side by side.
+constexpr int kTotalThreads = 1024;
+template <int W, int M> struct TotalShared {
+  double part[W][M];
+};
+// By a workgroup, in every thread.  (One wavefront took 0.7 us for each 512 terms: 270 of 453 us of a policy step of 200000 rows of 2000.)
+template <int M> __device__ __forceinline__ void block_totals(const double* const (&v)[M], int n, double (&t)[M]) {
+  constexpr int U = 8 / M, W = kTotalThreads / 64;
+  __shared__ TotalShared<W, M> sh;
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int m = 0; m < M; ++m) t[m] = 0.0;
+  for (int base = 0; base < n; base += U * kTotalThreads) {
+    double x[M][U];
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int i = base + k * kTotalThreads + tid;
+        x[m][k] = i < n ? v[m][i] : 0.0;
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) t[m] += x[m][k];
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    t[m] = wave_sum(t[m]);
+    if ((tid & 63) == 0) sh.part[tid >> 6][m] = t[m];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    t[m] = 0.0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) t[m] += sh.part[w][m];
+  }
+}
+// By a wavefront, of terms that come from other workgroups of the same launch: 64-bit words that say themselves that they are there (the
+// lowest bit of the fraction is set; a cleared word is 0), cleared as they are read.
 __device__ __forceinline__ double flagged_term(double v) { return __longlong_as_double(__double_as_longlong(v) | 1ll); }
-template <bool FRESH, int M> __device__ __forceinline__ void wave_total_of(double* const (&v)[M], int n, double (&t)[M]) {
+template <int M> __device__ __forceinline__ void fresh_totals(double* const (&v)[M], int n, double (&t)[M]) {
   constexpr int U = 8 / M;
   const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -153,7 +193,7 @@ template <bool FRESH, int M> __device__ __forceinline__ void wave_total_of(doubl
 #pragma unroll
         for (int k = 0; k < U; ++k) {
           const int i = base + k * 64 + lane;
-          x[m][k] = i < n ? (FRESH ? ld_agent(v[m] + i) : v[m][i]) : 0.0;
+          x[m][k] = i < n ? ld_agent(v[m] + i) : 0.0;
         }
       }
 #pragma unroll
@@ -163,7 +203,7 @@ template <bool FRESH, int M> __device__ __forceinline__ void wave_total_of(doubl
       }
       return __all(there) != 0;
     };
-    bool there = look() || !FRESH;
+    bool there = look();
     // (all had been sent when the last one was counted: this ends at once, unless calls that share a workspace have not been ordered)
     for (int polls = kWaitPolls; !there && polls > 0; --polls) there = look();
 #pragma unroll
@@ -171,33 +211,17 @@ template <bool FRESH, int M> __device__ __forceinline__ void wave_total_of(doubl
 #pragma unroll
       for (int k = 0; k < U; ++k) {
         t[m] += there ? x[m][k] : (double)NAN;
-        if (FRESH && base + k * 64 + lane < n) st_agent(v[m] + base + k * 64 + lane, 0.0);
+        if (base + k * 64 + lane < n) st_agent(v[m] + base + k * 64 + lane, 0.0);
       }
     }
   }
 #pragma unroll
   for (int m = 0; m < M; ++m) t[m] = wave_sum(t[m]);
 }
-template <bool FRESH> __device__ __forceinline__ double wave_total(double* v, int n) {
-  double* const p[1] = {v};
-  double t[1];
-  wave_total_of<FRESH, 1>(p, n, t);
-  return t[0];
-}
-template <bool FRESH> __device__ __forceinline__ void wave_totals(double* a, double* b, int n, double& ta, double& tb) {
-  double* const p[2] = {a, b};
-  double t[2];
-  wave_total_of<FRESH, 2>(p, n, t);
-  ta = t[0];
-  tb = t[1];
-}
 
-// A pair's loss and slope from the terms of its positions, by one wavefront (lane 0 writes).
-template <bool FRESH> __device__ __forceinline__ void settle_pair(const LossTerm& f, const LossWorkspace& ws, int i, int T) {
+// A pair's loss and slope from its sequences' scores (thread 0 writes).
+__device__ __forceinline__ void settle_pair(const LossTerm& f, const LossWorkspace& ws, int i, double chosen, double rejected) {
   const int P = f.P;
-  double* terms = FRESH ? ws.fresh : ws.term;
-  double chosen, rejected;
-  wave_totals<FRESH>(terms + (size_t)i * T, terms + (size_t)(P + i) * T, T, chosen, rejected);
   const double beta = (double)f.beta, e = (double)f.smoothing, D = chosen - rejected;
   double m, loss, slope;
   if (f.pair_kind == 1) {
@@ -221,7 +245,7 @@ template <bool FRESH> __device__ __forceinline__ void settle_pair(const LossTerm
   }
   const double w = f.pair_weight ? (double)f.pair_weight[i] : 1.0 / (double)P;
   const double scale = w * (f.grad_scale ? (double)*f.grad_scale : 1.0);
-  if ((threadIdx.x & 63) != 0) return;
+  if (threadIdx.x != 0) return;
   ws.pair[i] = w != 0.0 ? w * loss : 0.0;
   ws.seq[i] = w != 0.0 ? (float)(scale * slope) : 0.f;
   ws.seq[P + i] = w != 0.0 ? (float)(-scale * slope) : 0.f;
@@ -239,7 +263,7 @@ __device__ __forceinline__ bool last_of(int32_t* counter, int n) {
   set_arrival(counter, 0);
   return true;
 }
-// Position r is settled (one wavefront): the last of a pair settles the pair; without pairs the last of all adds up the loss.
+// Position r is settled (the workgroup's first wavefront): the last of a pair settles the pair; without pairs the last of all adds up the loss.
 __device__ __forceinline__ void position_done(const LossRows& rows, const LossTerm& f, const LossWorkspace& ws, int r, double term) {
   if (!f.loss) return;
   const bool first = (threadIdx.x & 63) == 0;
@@ -250,12 +274,18 @@ __device__ __forceinline__ void position_done(const LossRows& rows, const LossTe
   if (first) st_agent(ws.fresh + r, flagged_term(term));
   if (f.kind == kPreference) {
     const int b = r / rows.T, i = b < f.P ? b : b - f.P;
-    if (last_of(ws.done + 32 + i * ticket_stride(f.P, kAddsUp), 2 * rows.T)) settle_pair<true>(f, ws, i, rows.T);
+    if (!last_of(ws.done + 32 + i * ticket_stride(f.P, kAddsUp), 2 * rows.T)) return;
+    double* const v[2] = {ws.fresh + i * rows.T, ws.fresh + (f.P + i) * rows.T};
+    double score[2];
+    fresh_totals<2>(v, rows.T, score);
+    settle_pair(f, ws, i, score[0], score[1]);
     return;
   }
   if (!last_of(ws.done, rows.n)) return;
-  const double t = wave_total<true>(ws.fresh, rows.n);
-  if (first) *f.loss = (float)t;
+  double* const v[1] = {ws.fresh};
+  double t[1];
+  fresh_totals<1>(v, rows.n, t);
+  if (first) *f.loss = (float)t[0];
 }
 
 // Sums of the vectors v0 .. v1 of a row by one wavefront (where the slices' records did not arrive, which never happens to calls that are
@@ -271,9 +301,20 @@ template <int DT, bool REF> __device__ __noinline__ LossSums wave_sums(const cha
   return loss_fold_wave<REF>(a);
 }
 
+// The arrival words of the rows cut into slices: a set for each, however many there are (their last slices wait as those of few rows do: the
+// launch has nothing else to do meanwhile.  Counts / sets: log-probabilities of 303 rows of 32003 float 11.4 / 10.9 us, of 256 of 128256 bf16
+// of which 0.75 count 15.2 / 14.9, preference loss of 132 rows of 32003 bf16 15.9 / 15.1).
+struct SetArrivals {
+  uint64_t* base;
+  int row;
+  static constexpr int rows = 1;
+  __device__ __forceinline__ uint64_t* set() const { return base + row; }
+  __device__ __forceinline__ int32_t* count() const { return nullptr; }       // (of many rows)
+};
 // A slice's vectors come in batches of four per thread, the next batch on its way.
 constexpr int kSumsBatch = 4;
-template <int DT, bool REF, bool PAST> __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f, int S, int chunk, int early, LossWorkspace ws) {
+template <int DT, bool REF, bool PAST>
+__global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f, int S, int chunk, int early, LossWorkspace ws) {
   warm_kernargs<sizeof(LossRows) + sizeof(LossTerm) + 4 * sizeof(int) + sizeof(LossWorkspace)>();
   __shared__ LossSums sh[kWaves];
   const int r = blockIdx.x / S, s = blockIdx.x - r * S, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -340,7 +381,7 @@ template <int DT, bool REF, bool PAST> __global__ void __launch_bounds__(kBlock)
     uint64_t w[kXchgWords];
     bool arrived = true;
     pack_pair(PairRecord{a.m, a.s, a.u, REF ? a.mr : a.m, REF ? a.sr : 0.f, REF ? a.w : 0.f}, w);
-    if (!hand_off(PlainWords{ws.xchg + (size_t)r * S * kXchgWords}, s, S, Arrivals{ws.ticket, kTicketLossLen, r, rows.n}, f.wait, [] {}, w, arrived))
+    if (!hand_off(PlainWords{ws.xchg + (size_t)r * S * kXchgWords}, s, S, SetArrivals{ws.sets, r}, f.wait, [] {}, w, arrived))
       return;
     a = loss_empty();
     if (lane < S) {
@@ -356,11 +397,18 @@ template <int DT, bool REF, bool PAST> __global__ void __launch_bounds__(kBlock)
   position_done(rows, f, ws, r, term);
 }
 
-__global__ void __launch_bounds__(64) k_loss_pairs(LossTerm f, int T, LossWorkspace ws) { settle_pair<false>(f, ws, blockIdx.x, T); }
-
-__global__ void __launch_bounds__(64) k_loss_total(double* v, int n, float* out) {
-  const double t = wave_total<false>(v, n);
-  if (threadIdx.x == 0) *out = (float)t;
+__global__ void __launch_bounds__(kTotalThreads) k_loss_pairs(LossTerm f, int T, LossWorkspace ws) {
+  const int i = blockIdx.x;
+  const double* const v[2] = {ws.term + (size_t)i * T, ws.term + (size_t)(f.P + i) * T};
+  double score[2];
+  block_totals<2>(v, T, score);
+  settle_pair(f, ws, i, score[0], score[1]);
+}
+__global__ void __launch_bounds__(kTotalThreads) k_loss_total(const double* terms, int n, float* out) {
+  const double* const v[1] = {terms};
+  double t[1];
+  block_totals<1>(v, n, t);
+  if (threadIdx.x == 0) *out = (float)t[0];
 }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -449,6 +497,7 @@ __device__ __forceinline__ void emit_vec(char* out, int idx, int V, int x, const
 constexpr int kPiece = 8 * 64, kMostPieces = 2048;      // (2^20 rows: no more than 2^31 pieces)
 constexpr uint32_t kMostGroups = 1u << 22;
 constexpr int kResidentWaves = 8 * 4 * 256;
+constexpr int kGradAddsUp = 4096;     // pairs whose sum is formed beside the gradient, by one wavefront
 template <int DT, bool REF, bool PAST>
 __global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces, int per, LossWorkspace ws, int P, float* loss, int ent) {
   warm_kernargs<sizeof(LossRows) + 4 * sizeof(int) + sizeof(LossWorkspace) + sizeof(float*)>();
@@ -456,7 +505,9 @@ __global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces,
   const uint32_t step = (gridDim.x - (loss ? 1u : 0u)) * kWaves, units = (uint32_t)rows.n * (uint32_t)pieces;
   if (loss && blockIdx.x == gridDim.x - 1) {         // (the pairs' sum; its workgroup is one more than the rows take)
     if (threadIdx.x >= 64) return;
-    const double total = wave_total<false>(ws.pair, P);
+    double total = 0.0;
+    for (int i = lane; i < P; i += 64) total += ws.pair[i];
+    total = wave_sum(total);
     if (lane == 0) *loss = (float)total;
     return;
   }
@@ -543,7 +594,8 @@ __device__ __forceinline__ uint64_t send_results(uint64_t* at, int S, int own, c
 // Wavefronts per SIMD that the registers are limited for (64 of data and about 50 more: four; 16: eight).
 constexpr int join_waves(int nb, bool ref) { return !ref ? (nb <= 4 ? 8 : nb <= 8 ? 6 : 4) : (nb <= 2 ? 7 : nb <= 4 ? 5 : 4); }
 template <int DT, bool REF, int NB, int WPR, bool PAST>
-__global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(NB, REF)) k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, LossWorkspace ws) {
+__global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(NB, REF))
+k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, LossWorkspace ws) {
   warm_kernargs<sizeof(LossRows) + sizeof(LossTerm) + 4 * sizeof(int) + sizeof(LossWorkspace)>();
   constexpr int RPB = WPR < kWaves ? kWaves / WPR : 1, TR = 64 * WPR;          // rows per workgroup, threads per row
   __shared__ JoinShared<WPR < kWaves ? kWaves : WPR> sh;
@@ -623,7 +675,7 @@ __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(N
         bool arrived = true;
         uint64_t w[kXchgWords];
         pack_pair(PairRecord{a.m, a.s, a.u, REF ? a.mr : a.m, REF ? a.sr : 0.f, REF ? a.w : 0.f}, w);
-        settles = hand_off(PlainWords{words}, s, S, Arrivals{ws.sets, 0, r, rows.n, true}, f.wait,
+        settles = hand_off(PlainWords{words}, s, S, SetArrivals{ws.sets, r}, f.wait,
                            [&] {
                              if (s == S - 1) return;
                              in = ask_position(rows, f, r, b);
@@ -698,10 +750,6 @@ __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(N
     }
   }
 }
-
-}  // namespace
-
-namespace {
 
 // How k_loss_join cuts rows of nv vectors: wavefronts per row, vectors in registers per thread, slices (0: too long) and vectors per slice.
 //  * Few rows: as many slices as are resident together, of eight wavefronts and up to 8 vectors per thread (with a reference's row four
@@ -787,8 +835,8 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
     ADASD_LOSS_CASE(ADASD_F32, true, false) ADASD_LOSS_CASE(ADASD_BF16, false, true) ADASD_LOSS_CASE(ADASD_F32, false, true)
 #undef ADASD_LOSS_CASE
   }
-  const bool pairs = f.kind == kPreference;
-  if (pairs && n > 0 && !f.adds_up) launch_kernel(k_loss_pairs, dim3(f.P), dim3(64), st, f, rows.T, ws);
+  const bool pairs = f.kind == kPreference, grad_adds_up = pairs && grad && n > 0 && f.P <= kGradAddsUp;
+  if (pairs && n > 0 && !f.adds_up) launch_kernel(k_loss_pairs, dim3(f.P), dim3(kTotalThreads), st, f, rows.T, ws);
   if (grad && n > 0 && !(join && own_row)) {
     // as many vectors per lane as leave each resident wavefront a piece, up to 8
     const int64_t lanes = ((int64_t)n * nv + kResidentWaves - 1) / kResidentWaves;
@@ -796,19 +844,18 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
     const int per = max(fair, ((nv + kMostPieces - 1) / kMostPieces + 63) / 64 * 64), pieces = (nv + per - 1) / per;
     const uint32_t groups = ((uint32_t)n * (uint32_t)pieces + kWaves - 1) / kWaves;
     const bool last_past = bytes > kSumsPast;
-    const dim3 grid((groups < kMostGroups ? groups : kMostGroups) + (pairs ? 1 : 0));
+    const dim3 grid((groups < kMostGroups ? groups : kMostGroups) + (grad_adds_up ? 1 : 0));
 #define ADASD_GRAD_CASE(DTV, REFV, PASTV) \
     if (dt == DTV && by_ref == REFV && last_past == PASTV) \
-      launch_kernel((k_loss_grad<DTV, REFV, PASTV>), grid, block, st, rows, pieces, per, ws, pairs ? f.P : 0, pairs ? f.loss : nullptr, \
+      launch_kernel((k_loss_grad<DTV, REFV, PASTV>), grid, block, st, rows, pieces, per, ws, pairs ? f.P : 0, grad_adds_up ? f.loss : nullptr, \
                     ent ? 1 : 0);
     ADASD_GRAD_CASE(ADASD_BF16, false, false) ADASD_GRAD_CASE(ADASD_BF16, true, false) ADASD_GRAD_CASE(ADASD_F32, false, false)
     ADASD_GRAD_CASE(ADASD_F32, true, false) ADASD_GRAD_CASE(ADASD_BF16, false, true) ADASD_GRAD_CASE(ADASD_BF16, true, true)
     ADASD_GRAD_CASE(ADASD_F32, false, true) ADASD_GRAD_CASE(ADASD_F32, true, true)
 #undef ADASD_GRAD_CASE
   }
-  if (f.loss && (pairs ? n == 0 || !grad : !f.adds_up)) {
-    launch_kernel(k_loss_total, dim3(1), dim3(64), st, pairs ? ws.pair : ws.term, n == 0 ? 0 : pairs ? f.P : n, f.loss);
-  }
+  if (f.loss && (pairs ? !grad_adds_up : !f.adds_up))
+    launch_kernel(k_loss_total, dim3(1), dim3(kTotalThreads), st, (const double*)(pairs ? ws.pair : ws.term), n == 0 ? 0 : pairs ? f.P : n, f.loss);
   return hipGetLastError();
 }
 

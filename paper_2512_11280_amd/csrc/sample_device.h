@@ -117,10 +117,8 @@ struct PlainWords {
 struct Arrivals {
   int32_t* base;
   int len, row, rows;
-  bool sets = false;       // a set for each row of a launch of many, next to one another, too: their last slices then wait as those of few rows do
-  __device__ __forceinline__ bool waits() const { return sets || few_rows(rows); }
   __device__ __forceinline__ int32_t* count() const { return base + row * ticket_stride(rows, len); }                // (many rows)
-  __device__ __forceinline__ uint64_t* set() const { return reinterpret_cast<uint64_t*>(base + (sets ? 2 * (size_t)row : (size_t)row * 32)); }   // (few rows)
+  __device__ __forceinline__ uint64_t* set() const { return reinterpret_cast<uint64_t*>(base + row * 32); }          // (few rows)
 };
 static_assert(kFewRows * 32 <= kTicket1Len && kFewRows * 32 <= kTicket3Len, "a line of 128 bytes for each of few rows");
 // (lane 0 adds 1; what the word held before, in every lane)
@@ -170,16 +168,16 @@ __device__ __forceinline__ bool look_at_words(const uint64_t* words, uint64_t (&
 // for them all, which every slice adds to, it did: one after the other, the returned additions were what the kernel ended with,
 // 1 x 8 x 128256 bf16 14.9 -> 15.3 us a call; and so did records sent by an exchange, 32 x 128256 float 6.2 -> 7.3.  Giving a row up stands behind
 // the wait and not in its loop, where it lay in the way: 1 x 8 x 128256 15.0 -> 14.9.)
-template <class Slots, class Ask>
-__device__ __forceinline__ bool hand_off(const Slots& slots, int s, int S, const Arrivals& a, WordWait wait, const Ask& ask,
+template <class Slots, class Ask, class Arrival = Arrivals>
+__device__ __forceinline__ bool hand_off(const Slots& slots, int s, int S, const Arrival& a, WordWait wait, const Ask& ask,
                                          uint64_t (&w)[kXchgWords], bool& arrived) {
   const int lane = threadIdx.x & 63;
   const uint64_t w0 = w[0], w1 = w[1], w2 = w[2], word = lane == 0 ? w0 : lane == 1 ? w1 : w2;
   static_assert(kXchgWords == 3, "a lane per word");
   if (lane < kXchgWords) __hip_atomic_store(slots.at(s) + lane, word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const bool may_give_up = a.waits() && s == S - 1;
+  const bool may_give_up = few_rows(a.rows) && s == S - 1;
   if (!may_give_up) {
-    if (!a.waits()) {
+    if (!few_rows(a.rows)) {
       if (!last_to_add(add_arrival(a.count()), S)) return false;
       set_arrival(a.count(), 0);
     } else {
