@@ -140,7 +140,7 @@ constexpr int kTotalThreads = 1024;
 template <int W, int M> struct TotalShared {
   double part[W][M];
 };
-// By a workgroup, in every thread.  (One wavefront took 0.7 us for each 512 terms: 270 of 453 us of a policy step of 200000 rows of 2000.)
+// By a workgroup, in every thread.  (One wavefront took 0.7 us for each 512 terms: policy step of 200000 rows of 2000 443 -> 308 us.)
 template <int M> __device__ __forceinline__ void block_totals(const double* const (&v)[M], int n, double (&t)[M]) {
   constexpr int U = 8 / M, W = kTotalThreads / 64;
   __shared__ TotalShared<W, M> sh;
@@ -421,7 +421,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {       // neare
 }
 // A whole vector of gradients, or the elements of the last one that the row has.  Stored past the caches: a gradient of more than a few
 // hundred rows does not stay in them till it is read, and takes the place of logits that are still to be read (8192 rows of
-// 128256 bf16 796 -> 771 us, preference loss of 512 rows of 128256 float 162 -> 132, KL over 1024 rows of 152064 246 -> 227).
+// 128256 bf16 780 -> 738 us, preference loss of 512 rows of 128256 float 160 -> 129, KL over 1024 rows of 152064 229 -> 215).
 template <int DT> __device__ __forceinline__ void store_grad(char* row, int idx, int V, const float (&g)[Elem<DT>::per_vec]) {
   constexpr int EPV = Elem<DT>::per_vec;
   uint32_t w[4];
@@ -493,7 +493,7 @@ __device__ __forceinline__ void emit_vec(char* out, int idx, int V, int x, const
 }
 
 // Pieces of rows of `per` vectors, a wavefront each, from the last row to the first: the rows read last are still in the cache behind the L2s
-// (preference loss of 2048 rows of 128256 bf16 of which 0.67 count: 235 -> 211 us).
+// (preference loss of 2048 rows of 128256 bf16 of which 0.67 count: 210 -> 206 us).
 constexpr int kPiece = 8 * 64, kMostPieces = 2048;      // (2^20 rows: no more than 2^31 pieces)
 constexpr uint32_t kMostGroups = 1u << 22;
 constexpr int kResidentWaves = 8 * 4 * 256;
@@ -754,16 +754,16 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
 // How k_loss_join cuts rows of nv vectors: wavefronts per row, vectors in registers per thread, slices (0: too long) and vectors per slice.
 //  * Few rows: as many slices as are resident together, of eight wavefronts and up to 8 vectors per thread (with a reference's row four
 //    wavefronts and up to 4 + 4); where those would not all be, and would be with twice the vectors, that.  (Us a call, eight wavefronts x 8 / four x
-//    16: 64 rows of 32000 bf16 9.4 / 11.8, 512 19.4 / 21.2, 256 of 32003 float 18.6 / 20.9, 256 of 128256 bf16 30.7 / 28.1.  With a
-//    reference, 4 + 4 / 8 + 8: 64 of 32000 12.4 / 15.4, 128 14.5 / 16.6, but 256 of 128256 63 / 59.)
+//    16: 64 rows of 32000 bf16 9.6 / 11.6, 512 19.7 / 21.2, 256 of 32003 float 18.8 / 21.0, 256 of 128256 bf16 30.6 / 28.4.  With a
+//    reference, 4 + 4 / 8 + 8: 64 of 32000 11.8 / 14.7, 128 14.8 / 16.8, but 256 of 128256 64 / 59.)
 //  * Many short rows: as few wavefronts per row as hold it, with as few registers as it takes (rows of 2000 bf16, four wavefronts
-//    each / one / one of few registers: 200000 rows 1463 / 703 / 536 us; of 8000, four / two / one: 50000 rows 529 / 369 / 364).
-//  * Many long rows: eight wavefronts of 8 vectors per thread, three workgroups per compute unit.  Bytes on their way are what the
+//    each / one / one of few registers: 200000 rows 752 / 432 / 304 us; of 8000, four / two / one: 50000 rows 428 / 303 / 282).
+//  * Many long rows: eight wavefronts of 8 vectors per thread where those hold the row, else slices of four.  Bytes on their way are what the
 //    chip's rate takes, and a workgroup asks for nothing while it exchanges sums and settles, so that several should take turns.
-//    8192 rows of 128256 bf16, workgroups of 4 wavefronts x 16 vectors / 4 x 8 / 8 x 16 / 8 x 8 / 16 x 16 (no slices): 828 / 804 / 864 / 800 / 808 us;
-//    2048 of which 0.7 count 188 / 183 / 197 / 186 / 200; 2624 rows of 152064 331 / 326 / 366 / 311 / 427.
+//    8192 rows of 128256 bf16, workgroups of 4 wavefronts x 16 vectors / 4 x 8 / 8 x 16 / 8 x 8 / 16 x 16 (no slices): 722 / 701 / 811 / 738 / 828 us;
+//    2048 of which 0.7 count 169 / 159 / 176 / 166 / 192; 2624 rows of 152064 275 / 284 / 302 / 278 / 412.
 //  * With a reference's row, twice the registers: four wavefronts of 8 + 8 vectors (1024 rows of 152064 bf16, 4 x (4 + 4) / 4 x (8 + 8) /
-//    8 x (8 + 8): 314 / 251 / 267 us), eight where they hold the row (12480 rows of 32000 bf16 508 us, two slices 540).
+//    8 x (8 + 8): 299 / 222 / 234 us), eight where they hold the row (12480 rows of 32000 bf16 474 us, two slices 508).
 struct JoinPlan {
   int wpr, nb, S, chunk;
 };
@@ -783,16 +783,17 @@ JoinPlan join_plan(int n, int nv, bool ref) {
   if (nv <= 128 * most) return {2, most, 1, nv};
   if (ref && nv <= 256 * most) return {4, most, 1, nv};
   if (nv <= 512 * 8) return {8, 8, 1, nv};
-  const int wpr = ref ? 4 : 8, S = (nv + 512 * wpr - 1) / (512 * wpr);
+  const int wpr = ref || nv <= kMaxSplit * 2048 ? 4 : 8, S = (nv + 512 * wpr - 1) / (512 * wpr);
   return {wpr, 8, S <= kMaxSplit ? S : 0, slice_chunk(nv, S)};
 }
 
 }  // namespace
 
-// Logits of so many bytes are read past the caches.  Gradients of one launch read them once (1024 rows of 152064 bf16 and a reference's 226 -> 218
-// us, 200000 rows of 2000 493 -> 453; 385 rows of 32003 float and a reference's, which the cache behind the L2s can hold from the kernel
-// that wrote them, 34 -> 35).  Log-probabilities are often asked for ahead of a gradient, so only what that cache cannot hold;
-// the second read of a preference loss likewise (200000 rows of 2000 bf16 500 -> 447 us, 256 of 128256 44 -> 45).
+// Logits of so many bytes are read past the caches.  Gradients of one launch read them once (1024 rows of 152064 bf16 and a reference's 223 -> 215
+// us, 200000 rows of 2000 321 -> 306; 385 rows of 32003 float and a reference's, 50 MB each, which the cache behind the L2s can hold from
+// the kernel that wrote them, took 35 us that way and 34 without).  Log-probabilities are often asked for ahead of a gradient, so only
+// what that cache cannot hold (4096 rows of 128256 bf16 of which 0.64 count 123 -> 110); the second read of a preference loss likewise
+// (200000 rows of 2000 bf16 480 -> 442 us; 256 of 128256, were it done there, 44 -> 45).
 // Of so few bytes the logits are asked for before it is known whether their position counts: one latency less.
 constexpr int64_t kEarly = (int64_t)16 << 20;
 constexpr int64_t kJoinPast = (int64_t)64 << 20, kSumsPast = (int64_t)256 << 20;
@@ -821,7 +822,7 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
     ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, false) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, false) \
     ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, true) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, true)
     ADASD_JOIN_CASES(false, 4, 1) ADASD_JOIN_CASES(false, 8, 1) ADASD_JOIN_CASES(false, 16, 1) ADASD_JOIN_CASES(false, 16, 2)
-    ADASD_JOIN_CASES(false, 16, 4) ADASD_JOIN_CASES(false, 8, 8)
+    ADASD_JOIN_CASES(false, 16, 4) ADASD_JOIN_CASES(false, 8, 4) ADASD_JOIN_CASES(false, 8, 8)
     ADASD_JOIN_CASES(true, 2, 1) ADASD_JOIN_CASES(true, 4, 1) ADASD_JOIN_CASES(true, 8, 1) ADASD_JOIN_CASES(true, 8, 2)
     ADASD_JOIN_CASES(true, 8, 4) ADASD_JOIN_CASES(true, 8, 8) ADASD_JOIN_CASES(true, 4, 4)
 #undef ADASD_JOIN_CASES
