@@ -671,7 +671,8 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
         for (int n = 1; n < WPR; ++n) a = loss_merge<REF>(a, sh.sums[i * WPR + n]);
       }
       if (RPB == 1 && S > 1) {
-        a = loss_flagged<REF>(a);
+        a.m = odd_bit(a.m);
+        if (REF) a.mr = odd_bit(a.mr);
         bool arrived = true;
         uint64_t w[kXchgWords];
         pack_pair(PairRecord{a.m, a.s, a.u, REF ? a.mr : a.m, REF ? a.sr : 0.f, REF ? a.w : 0.f}, w);

@@ -17,7 +17,10 @@ struct LossSums {          // of a slice
   float m, s, u, w;        // of the row (w about the row's c)
   float mr, sr;            // of the reference's row
 };
-__device__ __forceinline__ LossSums loss_empty() { return LossSums{kNegHuge, 0.f, 0.f, 0.f, kNegHuge, 0.f}; }
+// Every reference has its lowest bit set (the flag of the hand-off words), from the first on: brought about afterwards it would cost each fold
+// a factor next to 1 and two roundings.
+__device__ __forceinline__ float odd_bit(float v) { return __uint_as_float(__float_as_uint(v) | 1u); }
+__device__ __forceinline__ LossSums loss_empty() { return LossSums{odd_bit(kNegHuge), 0.f, 0.f, 0.f, odd_bit(kNegHuge), 0.f}; }
 
 // One vector of the row (and of the reference's) joins a lane's sums, about the references that the sums have.  The vector's sums are
 // formed on their own, so that a chain of additions is one per vector long.
@@ -60,16 +63,16 @@ __device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const 
   }
 }
 
-// The sums about references that are at least as large as the logits of NV more vectors.
+// The sums about references that NV more vectors go by too: their largest logit, to a unit in the last place.
 template <int DT, bool REF, int NV>
 __device__ __forceinline__ void loss_raise(LossSums& a, const uint4 (&x)[NV], const uint4 (&xr)[NV]) {
-  const float m = fmaxf(a.m, vecs_max<DT, NV>(x)), d = a.m - m, f = ex2(d);
+  const float m = odd_bit(fmaxf(a.m, vecs_max<DT, NV>(x))), d = a.m - m, f = ex2(d);
   a.u = (a.u + d * a.s) * f;
   a.s *= f;
   a.m = m;
   if (REF) {
     a.w *= f;
-    const float mr = fmaxf(a.mr, vecs_max<DT, NV>(xr));
+    const float mr = odd_bit(fmaxf(a.mr, vecs_max<DT, NV>(xr)));
     a.sr *= ex2(a.mr - mr);
     a.mr = mr;
   }
@@ -92,33 +95,35 @@ template <bool REF> __device__ __forceinline__ LossSums loss_merge(const LossSum
   return r;
 }
 
-// The same sums about references whose lowest bit is set (the flag of the hand-off words).
-template <bool REF> __device__ __forceinline__ LossSums loss_flagged(const LossSums& a) {
-  LossSums r = a;
-  r.m = __uint_as_float(__float_as_uint(a.m) | 1u);
-  const float d = a.m > kNegHuge ? a.m - r.m : 0.f, f = ex2(d);
-  r.s = a.s * f;
-  r.u = (a.u + d * a.s) * f;
-  if (REF) {
-    r.w = a.w * f;
-    r.mr = __uint_as_float(__float_as_uint(a.mr) | 1u);
-    r.sr = a.sr * ex2(a.mr > kNegHuge ? a.mr - r.mr : 0.f);
-  }
-  return r;
+// Over the lanes of a wavefront in 64 bits, uniform.
+__device__ __forceinline__ double wave_sum_d(float v) {
+  double t = (double)v;
+  auto rotated = [&](auto rot) {
+    const uint64_t w = (uint64_t)__double_as_longlong(t);
+    const uint32_t lo = __float_as_uint(rot(__uint_as_float((uint32_t)w))), hi = __float_as_uint(rot(__uint_as_float((uint32_t)(w >> 32))));
+    return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+  };
+  t += rotated([](float x) { return dpp_rot<0x121>(x); });
+  t += rotated([](float x) { return dpp_rot<0x122>(x); });
+  t += rotated([](float x) { return dpp_rot<0x124>(x); });
+  t += rotated([](float x) { return dpp_rot<0x128>(x); });
+  auto of_row = [&](int lane) { return rotated([&](float x) { return lane_value(x, lane); }); };
+  return (of_row(0) + of_row(16)) + (of_row(32) + of_row(48));
 }
-// One wavefront folds its lanes' sums; uniform results, about references whose lowest bit is set (it is the flag of the hand-off words).
+// One wavefront folds its lanes' sums; uniform results.  The KL is the small difference of what s, sr and w say: these are folded in 64 bits
+// (six roundings fewer each).
 template <bool REF> __device__ __forceinline__ LossSums loss_fold_wave(const LossSums& a) {
   LossSums r = a;
-  const float top = wave_max_f(a.m);
-  r.m = __uint_as_float(__float_as_uint(top) | 1u);
-  const float d = top > kNegHuge ? a.m - r.m : 0.f, f = ex2(d);     // (nothing finite seen: the sums are 0, or a NaN)
-  r.s = wave_sum_f(a.s * f);
+  r.m = odd_bit(wave_max_f(a.m));                // (a NaN's lowest bit may be lost on the way)
+  const float d = a.m - r.m, f = ex2(d);
   r.u = wave_sum_f((a.u + d * a.s) * f);
   if (REF) {
-    r.w = wave_sum_f(a.w * f);
-    const float topr = wave_max_f(a.mr);
-    r.mr = __uint_as_float(__float_as_uint(topr) | 1u);
-    r.sr = wave_sum_f(a.sr * ex2(topr > kNegHuge ? a.mr - r.mr : 0.f));
+    r.s = (float)wave_sum_d(a.s * f);
+    r.w = (float)wave_sum_d(a.w * f);
+    r.mr = odd_bit(wave_max_f(a.mr));
+    r.sr = (float)wave_sum_d(a.sr * ex2(a.mr - r.mr));
+  } else {
+    r.s = wave_sum_f(a.s * f);
   }
   return r;
 }
