@@ -20,10 +20,11 @@ namespace {
 
 using namespace sampling;
 
-// A whole vector; PAST: without a place in the caches.
-template <bool PAST> __device__ __forceinline__ uint4 load_whole(const char* row, int idx) {
-  if (!PAST) return load_vec_any(row, idx);
-  const vec16_any v = __builtin_nontemporal_load(reinterpret_cast<const vec16_any*>(row + (size_t)idx * 16));
+// A whole vector, `lane` vectors behind one at a uniform place (the address then is that place and one register); PAST: without a place in the
+// caches.
+template <bool PAST> __device__ __forceinline__ uint4 load_whole(const char* row, int at, int lane) {
+  const vec16_any* from = reinterpret_cast<const vec16_any*>(row + (size_t)at * 16 + (uint32_t)lane * 16u);
+  const vec16_any v = PAST ? __builtin_nontemporal_load(from) : *from;
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
 template <int DT> __device__ __forceinline__ uint4 load_vec_of(const char* row, int idx, int V) {
@@ -119,10 +120,10 @@ __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const 
     k0 += by_kl * (kNat * (double)c - (row.lse - row.lse_ref) - row.kl);
     k.k2 = (float)(by_kl * kNat * row.inv_s);
   }
-  k.m = sums.m;
   k.c = c;
   k.a = (float)a;
   k.k0 = k0 == 0.0 ? 0.f : (float)(k0 * row.inv_s);      // (nothing of the row enters a gradient of zeros)
+  k.m = fabsf(k.k0) < INFINITY ? sums.m : __uint_as_float(0x7fc00001u);      // (every element of a gradient that is no number is none)
   return k;
 }
 
@@ -301,6 +302,17 @@ template <int DT, bool REF> __device__ __noinline__ LossSums wave_sums(const cha
   return loss_fold_wave<REF>(a);
 }
 
+// The elements behind the last whole vector join the first lane's sums.
+template <int DT, bool REF> __device__ __forceinline__ void push_tail(LossSums& a, const char* row, const char* ref, int V, float c) {
+  uint4 x[1] = {neutral_vec<DT>()}, xr[1] = {x[0]};
+  if ((threadIdx.x & 63) == 0) {
+    x[0] = load_last_vec<DT>(row, V);
+    xr[0] = REF ? load_last_vec<DT>(ref, V) : x[0];
+  }
+  loss_raise<DT, REF, 1>(a, x, xr);
+  loss_push_at<DT, REF>(a, x[0], xr[0], c);
+}
+
 // The arrival words of the rows cut into slices: a set for each, however many there are (their last slices wait as those of few rows do: the
 // launch has nothing else to do meanwhile.  Counts / sets: log-probabilities of 303 rows of 32003 float 11.4 / 10.9 us, of 256 of 128256 bf16
 // of which 0.75 count 15.2 / 14.9, preference loss of 132 rows of 32003 bf16 15.9 / 15.1).
@@ -323,20 +335,23 @@ __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f,
   PositionIn in = ask_position(rows, f, r, b);
   const char* row = row_at<DT>(rows.z, b, t);
   const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
-  const int nv = vectors_of<DT>(V), v0 = min(s * chunk, nv), v1 = min(v0 + chunk, nv);
-  const int whole = V / Elem<DT>::per_vec;
-  auto load = [&](const char* from, int idx) {
-    if (idx >= v1) return neutral_vec<DT>();
-    return idx < whole ? load_whole<PAST>(from, idx) : load_last_vec<DT>(from, V);
-  };
+  // whole vectors; one that is not is the first thread's of the last slice
+  const int whole = V / Elem<DT>::per_vec, v0 = min(s * chunk, whole), v1 = min(v0 + chunk, whole);
+  const bool tail = V % Elem<DT>::per_vec != 0 && s == S - 1 && wave == 0;
   uint4 next[kSumsBatch], nextr[kSumsBatch];
-  auto first_batch = [&] {
+  auto load_batch = [&](uint4 (&to)[kSumsBatch], const char* from, int base) {
+    if (base + kSumsBatch * kBlock <= v1) {
 #pragma unroll
-    for (int k = 0; k < kSumsBatch; ++k) next[k] = load(row, v0 + tid + k * kBlock);
-    if (REF) {
+      for (int k = 0; k < kSumsBatch; ++k) to[k] = load_whole<PAST>(from, base + k * kBlock, tid);
+    } else {
 #pragma unroll
-      for (int k = 0; k < kSumsBatch; ++k) nextr[k] = load(ref, v0 + tid + k * kBlock);
+      for (int k = 0; k < kSumsBatch; ++k)
+        to[k] = base + k * kBlock + tid < v1 ? load_whole<PAST>(from, base + k * kBlock, tid) : neutral_vec<DT>();
     }
+  };
+  auto first_batch = [&] {
+    load_batch(next, row, v0);
+    if (REF) load_batch(nextr, ref, v0);
   };
   if (early) first_batch();
   if (!position_counts(mark)) {
@@ -352,6 +367,7 @@ __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f,
   ask_logit<DT>(in, row, V);
   const float c = REF ? ref_shift<DT>(row, ref, in.x, V) : 0.f;
   LossSums a = loss_empty();
+  if (tail) push_tail<DT, REF>(a, row, ref, V, c);
   for (int base = v0; base < v1; base += kSumsBatch * kBlock) {
     uint4 x[kSumsBatch], xr[kSumsBatch];
 #pragma unroll
@@ -360,12 +376,8 @@ __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f,
       xr[k] = REF ? nextr[k] : next[k];
     }
     if (base + kSumsBatch * kBlock < v1) {
-#pragma unroll
-      for (int k = 0; k < kSumsBatch; ++k) {
-        const int idx = base + tid + (k + kSumsBatch) * kBlock;
-        next[k] = load(row, idx);
-        if (REF) nextr[k] = load(ref, idx);
-      }
+      load_batch(next, row, base + kSumsBatch * kBlock);
+      if (REF) load_batch(nextr, ref, base + kSumsBatch * kBlock);
     }
     loss_raise<DT, REF, kSumsBatch>(a, x, xr);
 #pragma unroll
@@ -389,7 +401,7 @@ __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f,
       a = LossSums{p.mp, p.sp, p.up, p.uq, p.mq, p.sq};
     }
     a = loss_fold_wave<REF>(a);
-    if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, nv, c);
+    if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, vectors_of<DT>(V), c);
   }
   double term;
   const LossCoef k = settle_position<REF>(rows, f, r, in, a, c, lane == 0, term);
@@ -422,21 +434,27 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {       // neare
 // A whole vector of gradients, or the elements of the last one that the row has.  Stored past the caches: a gradient of more than a few
 // hundred rows does not stay in them till it is read, and takes the place of logits that are still to be read (8192 rows of
 // 128256 bf16 780 -> 738 us, preference loss of 512 rows of 128256 float 160 -> 129, KL over 1024 rows of 152064 229 -> 215).
-template <int DT> __device__ __forceinline__ void store_grad(char* row, int idx, int V, const float (&g)[Elem<DT>::per_vec]) {
+template <int DT> __device__ __forceinline__ void grad_words(const float (&g)[Elem<DT>::per_vec], uint32_t (&w)[4]) {
   constexpr int EPV = Elem<DT>::per_vec;
-  uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (DT == ADASD_BF16) w[i] = pack_bf16(g[2 * i % EPV], g[(2 * i + 1) % EPV]);
     else w[i] = __float_as_uint(g[i]);
   }
-  if (idx < V / EPV) {
-    vec16_any v;
+}
+template <int DT> __device__ __forceinline__ void store_whole(char* row, int at, int lane, const float (&g)[Elem<DT>::per_vec]) {
+  uint32_t w[4];
+  grad_words<DT>(g, w);
+  vec16_any v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = w[i];
-    __builtin_nontemporal_store(v, reinterpret_cast<vec16_any*>(row + (size_t)idx * 16));
-    return;
-  }
+  for (int i = 0; i < 4; ++i) v[i] = w[i];
+  __builtin_nontemporal_store(v, reinterpret_cast<vec16_any*>(row + (size_t)at * 16 + (uint32_t)lane * 16u));
+}
+template <int DT> __device__ __forceinline__ void store_grad(char* row, int idx, int V, const float (&g)[Elem<DT>::per_vec]) {
+  constexpr int EPV = Elem<DT>::per_vec;
+  if (idx < V / EPV) return store_whole<DT>(row, idx, 0, g);
+  uint32_t w[4];
+  grad_words<DT>(g, w);
 #pragma unroll
   for (int i = 0; i < EPV - 1; ++i) {
     const int j = idx * EPV + i;
@@ -446,7 +464,7 @@ template <int DT> __device__ __forceinline__ void store_grad(char* row, int idx,
   }
 }
 
-// The gradients of one vector: a 1[j = x] + e (k0 + k1 t + k2 dd).
+// The gradients of one vector, but for the token's a: e (k0 + k1 t + k2 dd).  (Where e is 0 they are 0; a row whose k0 is no number has no m either.)
 template <int DT, bool ENT, bool REF>
 __device__ __forceinline__ void grad_vec(const uint4& x, const uint4& xr, const LossCoef& k, float (&g)[Elem<DT>::per_vec]) {
   const float neg_m = -k.m;
@@ -458,18 +476,15 @@ __device__ __forceinline__ void grad_vec(const uint4& x, const uint4& xr, const 
     for (int i = 0; i < 4; ++i) t[i] = fma_log2e(z[i], neg_m);
     ex2_group(t, e);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q[i] = ENT ? fmaf(k.k1, max_raw(t[i], -200.f), k.k0) : k.k0;
+    for (int i = 0; i < 4; ++i) q[i] = ENT ? fmaf(k.k1, t[i], k.k0) : k.k0;
     if (REF) {
       float y[4];
       unpack4<DT>(xr, h, y);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float dd = fma_log2e(z[i] - y[i], -k.c);
-        q[i] = fmaf(k.k2, e[i] > 0.f ? dd : 0.f, q[i]);
-      }
+      for (int i = 0; i < 4; ++i) q[i] = fmaf(k.k2, fma_log2e(z[i] - y[i], -k.c), q[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) g[4 * h + i] = e[i] * q[i];
+    for (int i = 0; i < 4; ++i) g[4 * h + i] = ENT || REF ? mass_times(e[i], q[i]) : e[i] * q[i];
   }
 }
 
@@ -480,11 +495,15 @@ template <int DT> __device__ __forceinline__ void zero_vec(char* row, int idx, i
   store_grad<DT>(row, idx, V, g);
 }
 template <int DT, bool REF>
+__device__ __forceinline__ void form_grad(const uint4& z, const uint4& zr, const LossCoef& k, bool ent, float (&g)[Elem<DT>::per_vec]) {
+  if (ent) grad_vec<DT, true, REF>(z, zr, k, g);
+  else grad_vec<DT, false, REF>(z, zr, k, g);
+}
+template <int DT, bool REF>
 __device__ __forceinline__ void emit_vec(char* out, int idx, int V, int x, const uint4& z, const uint4& zr, const LossCoef& k, bool ent) {
   constexpr int EPV = Elem<DT>::per_vec;
   float g[EPV];
-  if (ent) grad_vec<DT, true, REF>(z, zr, k, g);
-  else grad_vec<DT, false, REF>(z, zr, k, g);
+  form_grad<DT, REF>(z, zr, k, ent, g);
   if (idx == x / EPV) {
 #pragma unroll
     for (int i = 0; i < EPV; ++i) g[i] += idx * EPV + i == x ? k.a : 0.f;
@@ -530,7 +549,7 @@ __global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces,
     }
     const int x = rows.tokens[r];
     for (int idx = v0 + lane; idx < v1; idx += 64) {
-      const uint4 z = idx < V / Elem<DT>::per_vec ? load_whole<PAST>(row, idx) : load_last_vec<DT>(row, V);
+      const uint4 z = idx < V / Elem<DT>::per_vec ? load_whole<PAST>(row, idx, 0) : load_last_vec<DT>(row, V);
       emit_vec<DT, REF>(out, idx, V, x, z, REF ? load_vec_of<DT>(ref, idx, V) : z, k, ent);
     }
   }
@@ -599,7 +618,8 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
   warm_kernargs<sizeof(LossRows) + sizeof(LossTerm) + 4 * sizeof(int) + sizeof(LossWorkspace)>();
   constexpr int RPB = WPR < kWaves ? kWaves / WPR : 1, TR = 64 * WPR;          // rows per workgroup, threads per row
   __shared__ JoinShared<WPR < kWaves ? kWaves : WPR> sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), V = rows.V, nv = vectors_of<DT>(V);
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), V = rows.V;
+  constexpr int EPV = Elem<DT>::per_vec;
   const int r0 = RPB > 1 ? blockIdx.x * RPB : blockIdx.x / S, s = RPB > 1 ? 0 : blockIdx.x - r0 * S;
   const int sub = wave / WPR, r = r0 + sub, me = tid & (TR - 1);
   const bool here = r < rows.n;
@@ -609,7 +629,9 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
   int x = rows.tokens[r_here];
   const char* row = row_at<DT>(rows.z, b, t);
   const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
-  const int v0 = min(s * chunk, nv), v1 = min(v0 + chunk, nv);
+  // whole vectors; one that is not is the first thread's of the last slice
+  const int whole = V / EPV, v0 = min(s * chunk, whole), v1 = min(v0 + chunk, whole);
+  const bool tail = V % EPV != 0 && s == S - 1 && wave % WPR == 0;
   // what the positions are settled from, a pair of lanes for each row of the workgroup
   const int i = RPB > 1 ? min(lane >> 1, RPB - 1) : 0, ri = min(r0 + i, rows.n - 1), bi = ri / rows.T;
   PositionIn in{};
@@ -620,11 +642,10 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
   }
   uint4 v[NB], q[NB];
   auto load_row = [&] {
-    const int full = min(v1, V / Elem<DT>::per_vec);
     auto load = [&](const char* from, int j) {
-      const int idx = v0 + me + j * TR;
-      if (v0 + (j + 1) * TR <= full) return load_whole<PAST>(from, idx);
-      return idx < v1 ? load_vec_of<DT>(from, idx, V) : neutral_vec<DT>();
+      const int at = v0 + j * TR;
+      if (at + TR <= v1) return load_whole<PAST>(from, at, me);
+      return at + me < v1 ? load_whole<PAST>(from, at, me) : neutral_vec<DT>();
     };
 #pragma unroll
     for (int j = 0; j < NB; ++j) v[j] = load(row, j);
@@ -641,6 +662,7 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
   if (on) {
     if (REF) c = ref_shift<DT>(row, ref, x, V);
     LossSums a = loss_empty();
+    if (tail) push_tail<DT, REF>(a, row, ref, V, c);
     loss_raise<DT, REF, NB>(a, v, REF ? q : v);
 #pragma unroll
     for (int j = 0; j < NB; ++j)
@@ -690,7 +712,7 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
             a = LossSums{p.mp, p.sp, p.up, p.uq, p.mq, p.sq};
           }
           a = loss_fold_wave<REF>(a);
-          if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, nv, c);
+          if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, vectors_of<DT>(V), c);
         } else if (!await_result(results + s * kResultWords, f.wait, k)) {
           role = kLeaves;
         }
@@ -719,14 +741,32 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
   const LossCoef k = sh.coef[sub];
   // (beside the other wavefronts' part of the gradient)
   if (RPB == 1 && wave == 0 && (sh.role == kSettles || (!on && s == 0))) position_done(rows, f, ws, r, term);
+  int from = v0;
+  asm("" : "+s"(from));          // (else the places of the loads are kept in scalar registers for the stores, more than there are)
   if (out) {
+    const float none[EPV] = {};
     if (zero_row(k)) {
-      for (int idx = v0 + me; idx < v1; idx += TR) zero_vec<DT>(out, idx, V);
+      for (int at = from; at + me < v1; at += TR) store_whole<DT>(out, at, me, none);
+      if (tail && lane == 0) store_grad<DT>(out, whole, V, none);
     } else {
+      const int x_at = x >= 0 ? x / EPV : -1, x_in = x & (EPV - 1);       // (uniform)
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
-        const int idx = v0 + me + j * TR;
-        if (idx < v1) emit_vec<DT, REF>(out, idx, V, x, v[j], REF ? q[j] : v[j], k, ent);
+        const int at = from + j * TR;
+        if (at + me < v1) {
+          float g[EPV];
+          form_grad<DT, REF>(v[j], REF ? q[j] : v[j], k, ent, g);
+          if (x_at >= at && x_at < at + TR) {
+            const float a = x_at == at + me ? k.a : 0.f;
+#pragma unroll
+            for (int i = 0; i < EPV; ++i) g[i] += i == x_in ? a : 0.f;
+          }
+          store_whole<DT>(out, at, me, g);
+        }
+      }
+      if (tail && lane == 0) {          // (its logits, from memory again: nobody has put a gradient there)
+        const uint4 z = load_last_vec<DT>(row, V);
+        emit_vec<DT, REF>(out, whole, V, x, z, REF ? load_last_vec<DT>(ref, V) : z, k, ent);
       }
     }
   }
@@ -743,7 +783,7 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
   }
   __syncthreads();
   for (uint64_t left = sh.left; __builtin_expect(left != 0, 0); left &= left - 1) {
-    const int other = __ffsll((long long)left) - 1, u0 = min(other * chunk, nv), u1 = min(u0 + chunk, nv);
+    const int other = __ffsll((long long)left) - 1, nv = vectors_of<DT>(V), u0 = min(other * chunk, nv), u1 = other == S - 1 ? nv : min(u0 + chunk, nv);
 #pragma unroll 1
     for (int idx = u0 + tid; idx < u1; idx += TR) {
       const uint4 z = load_vec_of<DT>(row, idx, V);

@@ -22,13 +22,22 @@ struct LossSums {          // of a slice
 __device__ __forceinline__ float odd_bit(float v) { return __uint_as_float(__float_as_uint(v) | 1u); }
 __device__ __forceinline__ LossSums loss_empty() { return LossSums{odd_bit(kNegHuge), 0.f, 0.f, 0.f, odd_bit(kNegHuge), 0.f}; }
 
+// e v, and 0 where e is 0, whatever v is (a token without mass: v may be infinite, or no number).  One instruction; a comparison, a selection
+// and the product were three.
+__device__ __forceinline__ float mass_times(float e, float v) {
+  float r;
+  asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "v"(e), "v"(v));
+  return r;
+}
+
 // One vector of the row (and of the reference's) joins a lane's sums, about the references that the sums have.  The vector's sums are
 // formed on their own, so that a chain of additions is one per vector long.
 template <int DT, bool REF>
 __device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const uint4& xr, float c) {
   constexpr int EPV = Elem<DT>::per_vec;
   const float neg_m = -a.m, neg_mr = -a.mr;
-  float s[2] = {0.f, 0.f}, u[2] = {0.f, 0.f}, w[2] = {0.f, 0.f}, sr[2] = {0.f, 0.f};
+  float s[2], u[2], w[2], sr[2];
+  auto join = [](float& sum, float v, bool first) { sum = first ? v : sum + v; };
 #pragma unroll
   for (int g = 0; g < EPV / 4; ++g) {
     float z[4], t[4], e[4];
@@ -38,8 +47,9 @@ __device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const 
     ex2_group(t, e);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      s[i & 1] += e[i];
-      u[i & 1] = fmaf(max_raw(t[i], -200.f), e[i], u[i & 1]);      // (masked logits: (-200) * 0 = 0; a NaN stays one through e)
+      const float held = max_raw(t[i], -200.f);                    // (masked logits: (-200) * 0 = 0; a NaN stays one through e)
+      join(s[i & 1], e[i], g == 0 && i < 2);
+      u[i & 1] = g == 0 && i < 2 ? held * e[i] : fmaf(held, e[i], u[i & 1]);
     }
     if (REF) {
       float y[4], tr[4], er[4];
@@ -49,9 +59,8 @@ __device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const 
       ex2_group(tr, er);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        sr[i & 1] += er[i];
-        const float dd = fma_log2e(z[i] - y[i], -c);
-        w[i & 1] = fmaf(e[i], e[i] > 0.f ? dd : 0.f, w[i & 1]);    // (without mass nothing is added, whatever the reference has there)
+        join(sr[i & 1], er[i], g == 0 && i < 2);
+        join(w[i & 1], mass_times(e[i], fma_log2e(z[i] - y[i], -c)), g == 0 && i < 2);
       }
     }
   }
