@@ -792,7 +792,8 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
   }
 }
 
-// How k_loss_join cuts rows of nv vectors: wavefronts per row, vectors in registers per thread, slices (0: too long) and vectors per slice.
+// How k_loss_join cuts rows of nv vectors: wavefronts per row, vectors in registers per thread, slices (0: too long) and vectors per slice.  (Each line's
+// figures are of one build, the one it was decided in; later steps took 2 to 6 % off both sides.)
 //  * Few rows: as many slices as are resident together, of eight wavefronts and up to 8 vectors per thread (with a reference's row four
 //    wavefronts and up to 4 + 4); where those would not all be, and would be with twice the vectors, that.  (Us a call, eight wavefronts x 8 / four x
 //    16: 64 rows of 32000 bf16 9.6 / 11.6, 512 19.7 / 21.2, 256 of 32003 float 18.8 / 21.0, 256 of 128256 bf16 30.6 / 28.4.  With a
