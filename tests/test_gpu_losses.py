@@ -648,3 +648,52 @@ def test_two_graphs_on_one_workspace(am):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want)), k
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("V", [100, 4003, 70001])
+def test_gradients_that_are_no_numbers(am, V, dtype):
+    """A derivative that is no number makes every element of its row one, tokens without mass among them, and no element of another row."""
+    c = Case(2, 3, V, dtype, seed=41, masked=0.0)
+    z = c.z.clone()
+    z[..., ::3] = -math.inf
+    x = torch.full((2, 3), 1, dtype=torch.int32)
+    ws, one = c.ws(am), torch.ones(2, 3, device="cuda")
+
+    def rows_of_nan(g, *rows):
+        nan = torch.isnan(g.cpu().view(6, V))
+        assert [bool(r.all()) for r in nan] == [i in rows for i in range(6)] and [bool(r.any()) for r in nan] == [i in rows for i in range(6)]
+
+    nan = one.clone()
+    nan[0, 1] = math.nan
+    for a, h in ((nan, None), (one, nan), (nan, nan)):
+        rows_of_nan(am.token_logprob_grad(z.cuda(), x.cuda(), ws, a, h), 1)
+    inf = one.clone()
+    inf[1, 2] = math.inf
+    rows_of_nan(am.policy_loss(z.cuda(), x.cuda(), nan, ws, options=am.PolicyOptions(entropy_coef=0.1)).dlogits, 1)
+    rows_of_nan(am.policy_loss(z.cuda(), x.cuda(), one, ws, weight=inf, options=am.PolicyOptions(entropy_coef=0.1)).dlogits, 5)
+    zref = z.clone()
+    zref[0, 2, 2] = -math.inf                                  # the reference has no mass where the row has
+    for ent in (0.0, 0.1):
+        o = am.policy_loss(z.cuda(), x.cuda(), one, ws, ref_logits=zref.cuda(), options=am.PolicyOptions(kl_coef=0.1, entropy_coef=ent))
+        assert o.kl[0, 2].item() == math.inf
+        rows_of_nan(o.dlogits, 2)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("V", [100, 4003, 70001])
+def test_mass_that_is_lost_in_the_type(am, V, dtype):
+    """A probability below 2^-149 of the row's largest counts as 0, whatever the reference has there."""
+    c = Case(1, 4, V, dtype, seed=42, masked=0.0)
+    x = torch.full((1, 4), 1, dtype=torch.int32)
+    z, zref = c.z.clone(), (c.z.float() + 0.25 * c.n(*c.z.shape)).to(dtype)
+    z[..., 3::7] = -400.0
+    zref[:, 0::2, 3::7] = -math.inf
+    bare = z.clone()                                           # the same rows without those tokens
+    bare[..., 3::7] = -math.inf
+    opt = am.PolicyOptions(kl_coef=0.1, entropy_coef=0.1)
+    ws, one = c.ws(am), torch.ones(1, 4, device="cuda")
+    got, want = (am.policy_loss(a.cuda(), x.cuda(), one, ws, ref_logits=b.cuda(), options=opt) for a, b in ((z, zref), (bare, zref)))
+    assert torch.isfinite(got.kl).all() and not got.dlogits[..., 3::7].any() and not got.status.any()
+    for name in ("loss", "token_loss", "logprob", "entropy", "kl", "dlogits"):
+        assert torch.equal(getattr(got, name), getattr(want, name)), name
