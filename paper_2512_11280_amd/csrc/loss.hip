@@ -323,16 +323,31 @@ struct SetArrivals {
   __device__ __forceinline__ uint64_t* set() const { return base + row; }
   __device__ __forceinline__ int32_t* count() const { return nullptr; }       // (of many rows)
 };
+// The kernel's arguments, read again where they are needed (they are in the scalar cache).  Held from the start they are more than the scalar
+// registers, and each is put aside into a vector register and taken out again.
+template <class T> __device__ __forceinline__ T arguments_again() {
+  uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return scalar_load(reinterpret_cast<const T*>(at));
+}
+struct SumsArgs {
+  LossRows rows;
+  LossTerm f;
+  LossWorkspace ws;
+  int S, chunk, early;
+};
 // A slice's vectors come in batches of four per thread, the next batch on its way.
 constexpr int kSumsBatch = 4;
 template <int DT, bool REF, bool PAST>
-__global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f, int S, int chunk, int early, LossWorkspace ws) {
-  warm_kernargs<sizeof(LossRows) + sizeof(LossTerm) + 4 * sizeof(int) + sizeof(LossWorkspace)>();
+__global__ void __launch_bounds__(kBlock) k_loss_sums(SumsArgs args) {
+  warm_kernargs<sizeof(SumsArgs)>();
+  const LossRows& rows = args.rows;
+  const int S = args.S, chunk = args.chunk, early = args.early;
   __shared__ LossSums sh[kWaves];
   const int r = blockIdx.x / S, s = blockIdx.x - r * S, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = r / rows.T, t = r - b * rows.T, V = rows.V;
   const PositionMark mark = ask_mark(rows, r);
-  PositionIn in = ask_position(rows, f, r, b);
+  PositionIn in = ask_position(rows, args.f, r, b);
   const char* row = row_at<DT>(rows.z, b, t);
   const char* ref = REF ? row_at<DT>(rows.ref, b, t) : nullptr;
   // whole vectors; one that is not is the first thread's of the last slice
@@ -356,11 +371,12 @@ __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f,
   if (early) first_batch();
   if (!position_counts(mark)) {
     if (s != 0 || wave != 0) return;
+    const SumsArgs late = arguments_again<SumsArgs>();
     if (lane == 0) {
-      report_nothing(rows, f, r);
-      ws.coef[r] = LossCoef{};
+      report_nothing(late.rows, late.f, r);
+      late.ws.coef[r] = LossCoef{};
     }
-    position_done(rows, f, ws, r, 0.0);
+    position_done(late.rows, late.f, late.ws, r, 0.0);
     return;
   }
   if (!early) first_batch();
@@ -388,6 +404,9 @@ __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f,
   if (lane == 0) sh[wave] = a;
   __syncthreads();
   if (wave != 0) return;
+  const SumsArgs late = arguments_again<SumsArgs>();
+  const LossTerm& f = late.f;
+  const LossWorkspace& ws = late.ws;
   a = loss_fold_wave<REF>(lane < kWaves ? sh[lane] : loss_empty());
   if (S > 1) {
     uint64_t w[kXchgWords];
@@ -404,9 +423,9 @@ __global__ void __launch_bounds__(kBlock) k_loss_sums(LossRows rows, LossTerm f,
     if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, vectors_of<DT>(V), c);
   }
   double term;
-  const LossCoef k = settle_position<REF>(rows, f, r, in, a, c, lane == 0, term);
+  const LossCoef k = settle_position<REF>(late.rows, f, r, in, a, c, lane == 0, term);
   if (lane == 0) ws.coef[r] = k;
-  position_done(rows, f, ws, r, term);
+  position_done(late.rows, f, ws, r, term);
 }
 
 __global__ void __launch_bounds__(kTotalThreads) k_loss_pairs(LossTerm f, int T, LossWorkspace ws) {
@@ -610,12 +629,20 @@ __device__ __forceinline__ uint64_t send_results(uint64_t* at, int S, int own, c
   return __hip_atomic_exchange(at, record_word(bits_of(k.m), k.a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+struct JoinArgs {
+  LossRows rows;
+  LossTerm f;
+  LossWorkspace ws;
+  int S, chunk, ent, early;
+};
 // Wavefronts per SIMD that the registers are limited for (64 of data and about 50 more: four; 16: eight).
 constexpr int join_waves(int nb, bool ref) { return !ref ? (nb <= 4 ? 8 : nb <= 8 ? 6 : 4) : (nb <= 2 ? 7 : nb <= 4 ? 5 : 4); }
 template <int DT, bool REF, int NB, int WPR, bool PAST>
 __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(NB, REF))
-k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, LossWorkspace ws) {
-  warm_kernargs<sizeof(LossRows) + sizeof(LossTerm) + 4 * sizeof(int) + sizeof(LossWorkspace)>();
+k_loss_join(JoinArgs args) {
+  warm_kernargs<sizeof(JoinArgs)>();
+  const LossRows& rows = args.rows;
+  const int S = args.S, chunk = args.chunk, early = args.early;
   constexpr int RPB = WPR < kWaves ? kWaves / WPR : 1, TR = 64 * WPR;          // rows per workgroup, threads per row
   __shared__ JoinShared<WPR < kWaves ? kWaves : WPR> sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), V = rows.V;
@@ -637,7 +664,7 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
   PositionIn in{};
   PositionMark mark_i = mark;
   if (wave == 0 && s == S - 1) {
-    in = ask_position(rows, f, ri, bi);
+    in = ask_position(rows, args.f, ri, bi);
     if (RPB > 1) mark_i = ask_mark(rows, ri);
   }
   uint4 v[NB], q[NB];
@@ -678,9 +705,13 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
   double term = 0.0;
   bool settles = S == 1;
   uint64_t found = 0;
-  uint64_t* words = ws.xchg + (size_t)r * S * (kXchgWords + kResultWords);      // (S > 1: the records, then the results)
-  uint64_t* results = words + S * kXchgWords;
   if (wave == 0) {
+    const JoinArgs late = arguments_again<JoinArgs>();
+    const LossRows& rows = late.rows;
+    const LossTerm& f = late.f;
+    const LossWorkspace& ws = late.ws;
+    uint64_t* words = ws.xchg + (size_t)r * S * (kXchgWords + kResultWords);      // (S > 1: the records, then the results)
+    uint64_t* results = words + S * kXchgWords;
     LossCoef k{};
     int role = kWaitsFor;
     if (RPB > 1 || on) {
@@ -737,10 +768,12 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
   }
   __syncthreads();
   if (!here || (RPB == 1 && sh.role == kLeaves)) return;
-  char* out = rows.g.base ? const_cast<char*>(row_at<DT>(rows.g, b, t)) : nullptr;
+  const JoinArgs last = arguments_again<JoinArgs>();
+  const int ent = last.ent;
+  char* out = last.rows.g.base ? const_cast<char*>(row_at<DT>(last.rows.g, b, t)) : nullptr;
   const LossCoef k = sh.coef[sub];
   // (beside the other wavefronts' part of the gradient)
-  if (RPB == 1 && wave == 0 && (sh.role == kSettles || (!on && s == 0))) position_done(rows, f, ws, r, term);
+  if (RPB == 1 && wave == 0 && (sh.role == kSettles || (!on && s == 0))) position_done(last.rows, last.f, last.ws, r, term);
   int from = v0;
   asm("" : "+s"(from));          // (else the places of the loads are kept in scalar registers for the stores, more than there are)
   if (out) {
@@ -772,6 +805,7 @@ k_loss_join(LossRows rows, LossTerm f, int S, int chunk, int ent, int early, Los
   }
   if (RPB > 1 || S == 1 || !on || sh.role != kSettles) return;
   // ---- the slices that have ended without their results
+  uint64_t* results = last.ws.xchg + (size_t)r * S * (kXchgWords + kResultWords) + S * kXchgWords;
   if (wave == 0) {
     uint64_t left = __ballot(found == kLeft);
     if (lane == 0) sh.left = left;
@@ -858,8 +892,8 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
     const unsigned groups = plan.wpr >= kWaves ? n * plan.S : (n + kWaves / plan.wpr - 1) / (kWaves / plan.wpr);
 #define ADASD_JOIN_CASE(DTV, REFV, NBV, WPRV, PASTV) \
     if (dt == DTV && ref == REFV && plan.nb == NBV && plan.wpr == WPRV && past == PASTV) \
-      launch_kernel((k_loss_join<DTV, REFV, NBV, WPRV, PASTV>), dim3(groups), dim3(WPRV > kWaves ? 64 * WPRV : kBlock), st, some, f, plan.S, \
-                    plan.chunk, ent ? 1 : 0, early ? 1 : 0, ws);
+      launch_kernel((k_loss_join<DTV, REFV, NBV, WPRV, PASTV>), dim3(groups), dim3(WPRV > kWaves ? 64 * WPRV : kBlock), st, \
+                    JoinArgs{some, f, ws, plan.S, plan.chunk, ent ? 1 : 0, early ? 1 : 0});
 #define ADASD_JOIN_CASES(REFV, NBV, WPRV) \
     ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, false) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, false) \
     ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, true) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, true)
@@ -873,7 +907,7 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
     const int S = scan_split(n, rows.V, dt), chunk = slice_chunk(nv, S);
 #define ADASD_LOSS_CASE(DTV, REFV, PASTV) \
     if (dt == DTV && ref == REFV && past == PASTV) \
-      launch_kernel((k_loss_sums<DTV, REFV, PASTV>), dim3(n * S), block, st, rows, f, S, chunk, early ? 1 : 0, ws);
+      launch_kernel((k_loss_sums<DTV, REFV, PASTV>), dim3(n * S), block, st, SumsArgs{rows, f, ws, S, chunk, early ? 1 : 0});
     ADASD_LOSS_CASE(ADASD_BF16, false, false) ADASD_LOSS_CASE(ADASD_BF16, true, false) ADASD_LOSS_CASE(ADASD_F32, false, false)
     ADASD_LOSS_CASE(ADASD_F32, true, false) ADASD_LOSS_CASE(ADASD_BF16, false, true) ADASD_LOSS_CASE(ADASD_F32, false, true)
 #undef ADASD_LOSS_CASE
