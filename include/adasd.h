@@ -378,9 +378,9 @@ int adasd_update_thresholds(const adasd_state *st /* host */, int k_max, const i
  *   logprob[b,t]   = ln p(x);   entropy[b,t] = H(p) in nats (Appendix A of the paper);
  *   a position with weight[b,t] == 0 (or active[b,t] == 0) does not count: its logits, token and other inputs enter no result (they
  *   need not be numbers, or a token of the vocabulary), its results are 0, and its row of dlogits is written with zeros;
- *   status[b,t]    = ADASD_ST_BAD_TOKEN (token outside [0,V): log-probability NaN), ADASD_ST_NONFINITE (NaN, +inf or a logit of
- *                    2^120 or more in the row, or none above -2^120: results NaN), or 0.  A gradient row that depends on a NaN
- *                    is NaN.
+ *   status[b,t]    = ADASD_ST_BAD_TOKEN (token outside [0,V): log-probability NaN), ADASD_ST_NONFINITE (a NaN in the row, no
+ *                    finite logit, or a largest one beyond 2^26 in size: results NaN; a reference's row likewise), or 0.  A
+ *                    gradient row that depends on a NaN is NaN.
  * Logits of -inf, or of the type's lowest value beside ordinary ones, are tokens without mass: gradient 0 there.
  * Gradients have the type of the logits (formed in 32 bits, rounded once).  dlogits may be the logits' own memory (same pointer and
  * strides: the gradient takes their place); any other address range that overlaps that of logits the call reads is refused.

@@ -20,6 +20,8 @@ struct LossSums {          // of a slice
 // Every reference has its lowest bit set (the flag of the hand-off words), from the first on: brought about afterwards it would cost each fold
 // a factor next to 1 and two roundings.
 __device__ __forceinline__ float odd_bit(float v) { return __uint_as_float(__float_as_uint(v) | 1u); }
+// A row whose largest logit is beyond 2^26 in size is none of numbers here: a unit in the last place of m (8 at the border) is no small exponent.
+constexpr float kLargestM = 67108864.f * kLog2e + 16.f;
 __device__ __forceinline__ LossSums loss_empty() { return LossSums{odd_bit(kNegHuge), 0.f, 0.f, 0.f, odd_bit(kNegHuge), 0.f}; }
 
 // e v, and 0 where e is 0, whatever v is (a token without mass: v may be infinite, or no number).  One instruction; a comparison, a selection
@@ -72,7 +74,7 @@ __device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const 
   }
 }
 
-// The sums about references that NV more vectors go by too: their largest logit, to a unit in the last place.
+// The sums about references that NV more vectors go by too: their largest logit, to a unit in its last place.
 template <int DT, bool REF, int NV>
 __device__ __forceinline__ void loss_raise(LossSums& a, const uint4 (&x)[NV], const uint4 (&xr)[NV]) {
   const float m = odd_bit(fmaxf(a.m, vecs_max<DT, NV>(x))), d = a.m - m, f = ex2(d);
@@ -119,20 +121,18 @@ __device__ __forceinline__ double wave_sum_d(float v) {
   auto of_row = [&](int lane) { return rotated([&](float x) { return lane_value(x, lane); }); };
   return (of_row(0) + of_row(16)) + (of_row(32) + of_row(48));
 }
-// One wavefront folds its lanes' sums; uniform results.  The KL is the small difference of what s, sr and w say: these are folded in 64 bits
-// (six roundings fewer each).
+// One wavefront folds its lanes' sums; uniform results.  s (and sr and w, whose small difference the KL is) are folded in 64
+// bits, six roundings fewer each: the error of a log-probability 5.0e-8 rms for 6.5e-8, for 0.3 us of 14 in a call of 193 rows.
 template <bool REF> __device__ __forceinline__ LossSums loss_fold_wave(const LossSums& a) {
   LossSums r = a;
   r.m = odd_bit(wave_max_f(a.m));                // (a NaN's lowest bit may be lost on the way)
   const float d = a.m - r.m, f = ex2(d);
   r.u = wave_sum_f((a.u + d * a.s) * f);
+  r.s = (float)wave_sum_d(a.s * f);
   if (REF) {
-    r.s = (float)wave_sum_d(a.s * f);
     r.w = (float)wave_sum_d(a.w * f);
     r.mr = odd_bit(wave_max_f(a.mr));
     r.sr = (float)wave_sum_d(a.sr * ex2(a.mr - r.mr));
-  } else {
-    r.s = wave_sum_f(a.s * f);
   }
   return r;
 }
@@ -150,7 +150,7 @@ constexpr double kNat = 1.0 / (double)kLog2e;
 constexpr double kTemperature = (double)kLog2e * kLn2 - 1.0;
 template <bool REF> __device__ __forceinline__ LossRow finish_loss_row(const LossSums& t, float c) {
   LossRow r;
-  const bool ok = t.s > 0.f && t.s < INFINITY && fabsf(t.u) < INFINITY && t.m > kNegHuge && t.m < INFINITY;
+  const bool ok = t.s > 0.f && t.s < INFINITY && fabsf(t.u) < INFINITY && fabsf(t.m) <= kLargestM;
   const float s = ok ? t.s : NAN;
   const double l2 = log2_fine(s), inv = 1.0 / (double)s;
   r.H = fmax(kNat * (l2 - (double)t.u * inv), 0.0);
@@ -161,7 +161,7 @@ template <bool REF> __device__ __forceinline__ LossRow finish_loss_row(const Los
   r.lse_ref = 0.0;
   r.kl = 0.0;
   if (REF) {
-    const bool okr = t.sr > 0.f && t.sr < INFINITY && t.mr > kNegHuge && t.mr < INFINITY;
+    const bool okr = t.sr > 0.f && t.sr < INFINITY && fabsf(t.mr) <= kLargestM;
     const double l2r = log2_fine(okr ? t.sr : NAN);
     r.lse_ref = kNat * ((double)t.mr + l2r);
     // (c next to the normalisers' difference: both large where the rows carry different offsets)

@@ -697,3 +697,25 @@ def test_mass_that_is_lost_in_the_type(am, V, dtype):
     assert torch.isfinite(got.kl).all() and not got.dlogits[..., 3::7].any() and not got.status.any()
     for name in ("loss", "token_loss", "logprob", "entropy", "kl", "dlogits"):
         assert torch.equal(getattr(got, name), getattr(want, name)), name
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_the_largest_logits(am, dtype):
+    """Rows whose largest logit is up to 2^26 in size are right; beyond that they are flagged, whatever the rounding of their sums."""
+    B, T, V = 1, 16, 5000
+    g = torch.Generator().manual_seed(43)
+    noise, up = torch.randn(B, T, V, generator=g), 1.0 + 0.05 * torch.rand(B, T, generator=g)
+    x = torch.full((B, T), 7, dtype=torch.int32)
+    ws = am.LossWorkspace(B, T, V, dtype)
+    for size in (6.2e7, -6.2e7, 1e8, 1e9, -1e9, 1e30, -1e30):
+        z = noise.clone() if size > 0 else noise + size
+        if size > 0:
+            z[..., 7] = size * up
+        z = z.to(dtype)
+        lp, _, st = am.token_logprob(z.cuda(), x.cuda(), ws)
+        if abs(size) < 2.0**26:
+            # (equal logits, or one that takes all the mass: sums of up to 5000 equal terms, 13 roundings of half a unit)
+            R.near(lp, torch.log_softmax(z.double(), -1)[..., 7], 13 * 2.0**-24 + 2.0**-24 * 9.0)
+            assert not st.any()
+        else:
+            assert (st == 2).all() and torch.isnan(lp).all()
