@@ -178,8 +178,13 @@ template <int M> __device__ __forceinline__ void block_totals(const double* cons
   }
 }
 // By a wavefront, of terms that come from other workgroups of the same launch: 64-bit words that say themselves that they are there (the
-// lowest bit of the fraction is set; a cleared word is 0), cleared as they are read.
+// lowest bit of the fraction is set; a cleared word is 0), cleared as they are read.  An infinity travels as the signalling NaN of the bits one
+// above its own, which no term is (what arithmetic leaves is a quiet one).
 __device__ __forceinline__ double flagged_term(double v) { return __longlong_as_double(__double_as_longlong(v) | 1ll); }
+__device__ __forceinline__ double term_of(double flagged) {
+  const long long w = __double_as_longlong(flagged);
+  return (w & 0x7fffffffffffffffll) == 0x7ff0000000000001ll ? __longlong_as_double(w & ~1ll) : flagged;
+}
 template <int M> __device__ __forceinline__ void fresh_totals(double* const (&v)[M], int n, double (&t)[M]) {
   constexpr int U = 8 / M;
   const int lane = threadIdx.x & 63;
@@ -211,7 +216,7 @@ template <int M> __device__ __forceinline__ void fresh_totals(double* const (&v)
     for (int m = 0; m < M; ++m) {
 #pragma unroll
       for (int k = 0; k < U; ++k) {
-        t[m] += there ? x[m][k] : (double)NAN;
+        t[m] += there ? term_of(x[m][k]) : (double)NAN;
         if (base + k * 64 + lane < n) st_agent(v[m] + base + k * 64 + lane, 0.0);
       }
     }

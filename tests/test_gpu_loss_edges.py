@@ -1,0 +1,77 @@
+"""Losses over vocabulary rows at the edges of their inputs: infinite terms, masks of any finite value, rows that do not count beside broken
+ones, records that are not waited for.  Expected values are stated, or those of the 64-bit forms in loss_ref.py."""
+import math
+
+import pytest
+import torch
+
+import loss_ref as R
+from test_gpu_losses import BF, F, Case, am, cu  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+INF = math.inf
+
+# positions: a workgroup's own rows, a row in slices, more than one launch adds up beside a gradient, more than any launch adds up
+COUNTS = [(2, 3, 40), (2, 3, 32003), (4, 100, 9001), (20, 300, 40)]
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("shape", COUNTS)
+def test_an_infinite_term_makes_the_loss_infinite(am, shape, dtype):  # noqa: F811
+    """A KL of +inf (the reference has no mass where the row has) in the policy loss, however the terms are added up."""
+    c = Case(*shape, dtype, seed=51, masked=0.0)
+    zref = c.z.clone()
+    zref[0, 1, 5] = -INF
+    one = torch.ones(c.B, c.T, device="cuda")
+    ws, opt = c.ws(am), am.PolicyOptions(kl_coef=0.1)
+    for need_grad in (True, False):
+        for sign in (1.0, -1.0):
+            o = am.policy_loss(c.z.cuda(), c.x.cuda(), one, ws, weight=sign * one, ref_logits=zref.cuda(), options=opt, need_grad=need_grad)
+            assert o.token_loss[0, 1].item() == INF and o.loss.item() == sign * INF
+    w = one.clone()
+    w[0, 1] = -1.0
+    zref[1, 2, 5] = -INF
+    o = am.policy_loss(c.z.cuda(), c.x.cuda(), one, ws, weight=w, ref_logits=zref.cuda(), options=opt)
+    assert math.isnan(o.loss.item())                                               # inf - inf
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("side", ["chosen", "rejected"])
+@pytest.mark.parametrize("shape", [(2, 3, 40), (4, 5, 32003), (4, 1030, 40), (4, 1030, 1037)])
+def test_a_token_without_mass_in_a_pair(am, shape, side, dtype):  # noqa: F811
+    """Log-probability -inf in the second pair: scores, losses and slopes as the formulas have them, below and above 4096 positions."""
+    c = Case(*shape, dtype, seed=52, masked=0.0)
+    B, T, V = shape
+    P = B // 2
+    b, t = (P - 1 if side == "chosen" else B - 1), T // 2
+    z = c.z.clone()
+    x = int(c.x[b, t])
+    z[b, t, x] = -INF
+    o = R.rows(z, c.x)
+    beta, ws = 0.125, c.ws(am)
+    for kind, e in (("logistic", 0.0), ("logistic", 0.25), ("hinge", 0.0), ("squared", 0.0)):
+        r = am.preference_loss(z.cuda(), c.x.cuda(), ws, options=am.PreferenceOptions(kind=kind, beta=beta, label_smoothing=e))
+        m = -INF if side == "chosen" else INF
+        if kind == "squared":
+            loss, slope = INF, 2.0 * m
+        elif kind == "hinge":
+            loss, slope = (INF, -beta) if side == "chosen" else (0.0, 0.0)
+        else:
+            loss = (INF if side == "chosen" or e > 0 else 0.0)
+            slope = -beta * (1.0 - e) if side == "chosen" else beta * e
+        assert r.logprob[b, t].item() == -INF and r.score[b].item() == -INF and torch.isfinite(r.score).sum().item() == B - 1
+        assert r.margin[P - 1].item() == m and r.pair_loss[P - 1].item() == loss, (kind, r.margin, r.pair_loss)
+        others = r.pair_loss.cpu()[:P - 1]
+        assert torch.isfinite(others).all()
+        assert r.loss.item() == INF if loss == INF else abs(r.loss.item() - others.double().sum().item() / P) <= 4 * R.H24 * others.double().sum().item()
+        both = [P - 1, B - 1]
+        if math.isinf(slope):
+            assert not torch.isfinite(r.dlogits[b, t, x]).item()
+            continue
+        a = torch.zeros(B, T, dtype=torch.float64)
+        a[P - 1], a[B - 1] = slope / P, -slope / P
+        g, tol = R.grad({k: v[both] if torch.is_tensor(v) else v for k, v in o.items()}, a[both], dtype=dtype)
+        R.near(r.dlogits[both], g, tol, f"dlogits {kind}")
+        if slope == 0.0:
+            assert not r.dlogits[both].any()
