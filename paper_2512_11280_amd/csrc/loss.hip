@@ -558,7 +558,7 @@ __global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces,
     const uint32_t back = units - 1 - unit;
     const int r = (int)(back / (uint32_t)pieces), piece = (int)(back - (uint32_t)r * (uint32_t)pieces), b = r / rows.T, t = r - b * rows.T;
     LossCoef k = scalar_load(ws.coef + r);
-    if (P > 0) {                       // (a pair's slope, sequence by sequence)
+    if (P > 0 && !zero_row(k)) {       // (a pair's slope, sequence by sequence; it may be no number, and this position one that does not count)
       const float d = scalar_load(ws.seq + b);
       k.a = d == 0.f ? 0.f : k.a * d;
       k.k0 = d == 0.f ? 0.f : k.k0 * d;

@@ -75,3 +75,21 @@ def test_a_token_without_mass_in_a_pair(am, shape, side, dtype):  # noqa: F811
         R.near(r.dlogits[both], g, tol, f"dlogits {kind}")
         if slope == 0.0:
             assert not r.dlogits[both].any()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("kind", ["logistic", "squared"])
+def test_rows_that_do_not_count_in_a_broken_pair(am, kind, dtype):  # noqa: F811
+    """Zeros, although the pair's slope is no number (a NaN row), or infinite (the squared loss of a token without mass)."""
+    for B, T, V in ((2, 6, 40), (4, 5, 32003), (4, 1100, 40)):
+        c = Case(B, T, V, dtype, seed=53, masked=0.5)
+        w = (c.w != 0).float()
+        w[0, 0], w[0, 1], w[B // 2, 2] = 1.0, 0.0, 0.0
+        for broken in (math.nan, -INF):
+            z = c.z.clone()
+            z[0, 0, int(c.x[0, 0])] = broken
+            z[w == 0] = math.nan
+            o = am.preference_loss(z.cuda(), c.x.cuda(), c.ws(am), weight=w.cuda(), options=am.PreferenceOptions(kind=kind))
+            assert not o.dlogits.cpu()[w == 0].any(), (B, T, V, broken)
+            if math.isnan(broken):
+                assert torch.isnan(o.dlogits.cpu()[0, 0]).all()
