@@ -22,7 +22,13 @@ struct LossSums {          // of a slice
 __device__ __forceinline__ float odd_bit(float v) { return __uint_as_float(__float_as_uint(v) | 1u); }
 // A row whose largest logit is beyond 2^26 in size is none of numbers here: a unit in the last place of m (8 at the border) is no small exponent.
 constexpr float kLargestM = 67108864.f * kLog2e + 16.f;
-__device__ __forceinline__ LossSums loss_empty() { return LossSums{odd_bit(kNegHuge), 0.f, 0.f, 0.f, odd_bit(kNegHuge), 0.f}; }
+// The lowest reference of any part of a row, below -kLargestM: a row that ends with it is none of numbers either.  Logits far below it (masks, of
+// whatever finite value) have no mass about it, and a part of a row that holds nothing else stays at 0.  Were references to follow such
+// logits, they would be off by up to a unit in their last place, which from 2^31 on is an exponent past the type's range; and the difference of two
+// of them times a sum would pass it in the folds.  (-2^27: a unit is 16 there, e at most 2^24.)
+constexpr float kLowestM = -134217728.f;
+static_assert(kLowestM < -kLargestM, "a row at the lowest reference is flagged");
+__device__ __forceinline__ LossSums loss_empty() { return LossSums{odd_bit(kLowestM), 0.f, 0.f, 0.f, odd_bit(kLowestM), 0.f}; }
 
 // e v, and 0 where e is 0, whatever v is (a token without mass: v may be infinite, or no number).  One instruction; a comparison, a selection
 // and the product were three.
@@ -96,7 +102,7 @@ template <bool REF> __device__ __forceinline__ LossSums loss_merge(const LossSum
   r.s = a.s * fa + b.s * fb;
   r.u = (a.u + da * a.s) * fa + (b.u + db * b.s) * fb;
   r.w = 0.f;
-  r.mr = kNegHuge;
+  r.mr = kLowestM;
   r.sr = 0.f;
   if (REF) {
     r.w = a.w * fa + b.w * fb;

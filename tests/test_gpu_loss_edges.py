@@ -93,3 +93,45 @@ def test_rows_that_do_not_count_in_a_broken_pair(am, kind, dtype):  # noqa: F811
             assert not o.dlogits.cpu()[w == 0].any(), (B, T, V, broken)
             if math.isnan(broken):
                 assert torch.isnan(o.dlogits.cpu()[0, 0]).all()
+
+
+# Finite values that serve as masks, all far below the ordinary logits' 149 binary orders: the tokens have no mass, as with -inf.
+MASKS = {BF: [-1e4, -1e9, -1.5e9, -1e10, -3e12, -1e30, -2.5e36, -1e38, -2e38, torch.finfo(BF).min],
+         F: [-1e4, -1e9, -1.5e9, -1e10, -3e12, -1e30, -5e36, -1e37, -1e38, -2e38, torch.finfo(F).min / 2, torch.finfo(F).min]}
+
+
+@pytest.mark.parametrize("dtype, mask", [(d, m) for d in (BF, F) for m in MASKS[d]])
+def test_masks_of_any_size(am, mask, dtype):  # noqa: F811
+    """Whole stretches of the vocabulary masked with one value, longer than any lane's, wavefront's or slice's part, and single tokens: bit for bit
+    what -inf gives, in every cut of the rows, in the forward pass and in the gradients, with a reference masked alike and without."""
+    one = None
+    for B, T, V in ((1, 1, 128256), (3, 5, 9001), (2, 2, 40), (31, 43, 1037), (2, 600, 20011)):
+        c = Case(B, T, V, dtype, seed=54, masked=0.0)
+        zref = (c.z.float() + 0.5 * c.n(B, T, V)).to(dtype)
+        x = c.x.clone()
+
+        def masked(value):
+            z, q = c.z.clone(), zref.clone()
+            for v in (z, q):
+                keep = v.gather(-1, x.long()[..., None]).clone()
+                v[..., V // 5:V // 5 + V // 2] = value
+                v[..., 1::7] = value
+                v.scatter_(-1, x.long()[..., None], keep)
+            return z.cuda(), q.cuda()
+        one = torch.ones(B, T, device="cuda")
+        ws = c.ws(am)
+
+        def call(value):
+            z, q = masked(value)
+            lp, H, st = am.token_logprob(z, x.cuda(), ws)
+            g = am.token_logprob_grad(z, x.cuda(), ws, one, one)
+            o = am.policy_loss(z, x.cuda(), one, ws, ref_logits=q, options=am.PolicyOptions(kl_coef=0.1, entropy_coef=0.1))
+            r = [lp, H, st, g, o.loss, o.token_loss, o.kl, o.dlogits, o.status]
+            if B % 2 == 0:
+                p = am.preference_loss(z, x.cuda(), ws)
+                r += [p.loss, p.score, p.dlogits]
+            return r
+        want, got = call(-INF), call(mask)
+        assert not got[2].any() and not got[8].any(), (B, T, V)
+        for k, (a, b) in enumerate(zip(got, want)):
+            assert torch.isfinite(a).all() and torch.equal(a, b), (B, T, V, k)
