@@ -381,6 +381,9 @@ __device__ __forceinline__ float wave_sum4(float a, float b, float c, float d) {
   return row_sum16(x + y);
 }
 
+// Maxima leave NaNs out, signalling ones too.  With the mode's IEEE bit, which is set when a kernel starts, the larger of a signalling NaN and x is the
+// NaN made a quiet one, and x is lost.  (At the top of a kernel, ahead of the loads of what is compared.)
+__device__ __forceinline__ void maxima_without_nans() { asm volatile("s_setreg_imm32_b32 hwreg(HW_REG_MODE, 9, 1), 0" ::: "memory"); }
 __device__ __forceinline__ uint32_t pk_max_f16(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
@@ -394,7 +397,8 @@ template <int DT> __device__ __forceinline__ uint4 neutral_vec() {   // all logi
 
 // Largest finite logit held in NV vectors, times log2(e) (kNegHuge if there is none).
 // bf16 pairs are compared as packed f16: both formats order their bit patterns the same way, and
-// the bf16 patterns of +-inf / NaN read as f16 NaNs, which the packed max ignores.
+// the bf16 patterns of +-inf / NaN and of anything from 2^121 on in size read as f16 NaNs, which the packed max ignores (those below 2^125 are
+// signalling ones: see maxima_without_nans).
 template <int DT, int NV> __device__ __forceinline__ float vecs_max(const uint4 (&v)[NV]) {
   if (DT == ADASD_BF16) {
     uint32_t m = pk_max_f16(v[0].x, v[0].y);

@@ -345,6 +345,7 @@ struct SumsArgs {
 constexpr int kSumsBatch = 4;
 template <int DT, bool REF, bool PAST>
 __global__ void __launch_bounds__(kBlock) k_loss_sums(SumsArgs args) {
+  maxima_without_nans();
   warm_kernargs<sizeof(SumsArgs)>();
   const LossRows& rows = args.rows;
   const int S = args.S, chunk = args.chunk, early = args.early;
@@ -645,6 +646,7 @@ constexpr int join_waves(int nb, bool ref) { return !ref ? (nb <= 4 ? 8 : nb <= 
 template <int DT, bool REF, int NB, int WPR, bool PAST>
 __global__ void __launch_bounds__(WPR > kWaves ? 64 * WPR : kBlock, join_waves(NB, REF))
 k_loss_join(JoinArgs args) {
+  maxima_without_nans();
   warm_kernargs<sizeof(JoinArgs)>();
   const LossRows& rows = args.rows;
   const int S = args.S, chunk = args.chunk, early = args.early;

@@ -96,7 +96,7 @@ def test_rows_that_do_not_count_in_a_broken_pair(am, kind, dtype):  # noqa: F811
 
 
 # Finite values that serve as masks, all far below the ordinary logits' 149 binary orders: the tokens have no mass, as with -inf.
-MASKS = {BF: [-1e4, -1e9, -1.5e9, -1e10, -3e12, -1e30, -2.5e36, -1e38, -2e38, torch.finfo(BF).min],
+MASKS = {BF: [-1e4, -1e9, -1.5e9, -1e10, -3e12, -1e30, -2.5e36, -5e36, -9e36, -2e37, -1e38, -2e38, torch.finfo(BF).min],
          F: [-1e4, -1e9, -1.5e9, -1e10, -3e12, -1e30, -5e36, -1e37, -1e38, -2e38, torch.finfo(F).min / 2, torch.finfo(F).min]}
 
 
