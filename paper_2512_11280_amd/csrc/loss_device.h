@@ -30,7 +30,7 @@ constexpr float kLowestM = -134217728.f;
 static_assert(kLowestM < -kLargestM, "a row at the lowest reference is flagged");
 __device__ __forceinline__ LossSums loss_empty() { return LossSums{odd_bit(kLowestM), 0.f, 0.f, 0.f, odd_bit(kLowestM), 0.f}; }
 
-// e v, and 0 where e is 0, whatever v is (a token without mass: v may be infinite, or no number).  One instruction; a comparison, a selection
+// e v, and 0 where e is 0, whatever v is (a token, or a part of a row, without mass: v may be infinite, or no number).  One instruction; a comparison, a selection
 // and the product were three.
 __device__ __forceinline__ float mass_times(float e, float v) {
   float r;
@@ -88,7 +88,7 @@ __device__ __forceinline__ void loss_raise(LossSums& a, const uint4 (&x)[NV], co
   a.s *= f;
   a.m = m;
   if (REF) {
-    a.w *= f;
+    a.w = mass_times(f, a.w);
     const float mr = odd_bit(fmaxf(a.mr, vecs_max<DT, NV>(xr)));
     a.sr *= ex2(a.mr - mr);
     a.mr = mr;
@@ -105,7 +105,7 @@ template <bool REF> __device__ __forceinline__ LossSums loss_merge(const LossSum
   r.mr = kLowestM;
   r.sr = 0.f;
   if (REF) {
-    r.w = a.w * fa + b.w * fb;
+    r.w = mass_times(fa, a.w) + mass_times(fb, b.w);
     r.mr = fmaxf(a.mr, b.mr);
     r.sr = a.sr * ex2(a.mr - r.mr) + b.sr * ex2(b.mr - r.mr);
   }
@@ -136,7 +136,7 @@ template <bool REF> __device__ __forceinline__ LossSums loss_fold_wave(const Los
   r.u = wave_sum_f((a.u + d * a.s) * f);
   r.s = (float)wave_sum_d(a.s * f);
   if (REF) {
-    r.w = (float)wave_sum_d(a.w * f);
+    r.w = (float)wave_sum_d(mass_times(f, a.w));
     r.mr = odd_bit(wave_max_f(a.mr));
     r.sr = (float)wave_sum_d(a.sr * ex2(a.mr - r.mr));
   }

@@ -135,3 +135,21 @@ def test_masks_of_any_size(am, mask, dtype):  # noqa: F811
         assert not got[2].any() and not got[8].any(), (B, T, V)
         for k, (a, b) in enumerate(zip(got, want)):
             assert torch.isfinite(a).all() and torch.equal(a, b), (B, T, V, k)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_kl_of_stretches_whose_mass_is_lost(am, dtype):  # noqa: F811
+    """Stretches of tokens below 2^-149 of the row's largest, of which the reference has none: they count as 0, whoever adds them up."""
+    for B, T, V in ((1, 2, 128256), (3, 5, 9001), (31, 43, 1037), (2, 600, 20011)):
+        c = Case(B, T, V, dtype, seed=56, masked=0.0)
+        x = torch.full((B, T), 1, dtype=torch.int32)
+        z, zref = c.z.clone(), (c.z.float() + 0.25 * c.n(B, T, V)).to(dtype)
+        at = slice(V // 5, V // 5 + V // 2)
+        z[..., at], zref[..., at] = -400.0, -INF
+        bare = z.clone()
+        bare[..., at] = -INF
+        opt, ws, one = am.PolicyOptions(kl_coef=0.1, entropy_coef=0.1), c.ws(am), torch.ones(B, T, device="cuda")
+        got, want = (am.policy_loss(a.cuda(), x.cuda(), one, ws, ref_logits=zref.cuda(), options=opt) for a in (z, bare))
+        assert torch.isfinite(got.kl).all() and torch.isfinite(got.dlogits).all() and not got.status.any()
+        for name in ("loss", "token_loss", "logprob", "entropy", "kl", "dlogits"):
+            assert torch.equal(getattr(got, name), getattr(want, name)), name
