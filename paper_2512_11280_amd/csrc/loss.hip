@@ -30,14 +30,6 @@ template <bool PAST> __device__ __forceinline__ uint4 load_whole(const char* row
 template <int DT> __device__ __forceinline__ uint4 load_vec_of(const char* row, int idx, int V) {
   return idx < V / Elem<DT>::per_vec ? load_vec_any(row, idx) : load_last_vec<DT>(row, V);
 }
-// The reference c of a row: what the logits of its token differ by, if that is a number (any value would do; near the typical
-// difference the sums about it cancel least).
-template <int DT> __device__ __forceinline__ float ref_shift(const char* row, const char* ref, int x, int V) {
-  const int at = x >= 0 && x < V ? x : 0;
-  const float d = (load_elem<DT>(row, at) - load_elem<DT>(ref, at)) * kLog2e;
-  return fabsf(d) < INFINITY ? d : 0.f;
-}
-
 // What the numbers of a position are formed from, asked for ahead of the row.
 struct PositionIn {
   float z, weight, a, h, old, ref;      // logit of the token; a: advantage or dlogprob; h: dentropy
@@ -65,10 +57,11 @@ template <int DT> __device__ __forceinline__ void ask_logit(PositionIn& in, cons
 // pairs of them) go through it together; the one that `writes` reports.
 template <bool REF>
 __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const LossTerm& f, int r, const PositionIn& in, const LossSums& sums,
-                                                    float c, bool writes, double& term) {
+                                                    bool writes, double& term) {
   const bool odd = threadIdx.x & 1;
   const bool known = in.x >= 0 && in.x < rows.V;
-  const LossRow row = finish_loss_row<REF>(sums, c);
+  const LossRow row = finish_loss_row<REF>(sums);
+  const float c = REF ? c_of(sums.m, sums.mr) : 0.f;
   const double lp = known ? (double)in.z - row.lse : (double)NAN;
   const double w = (double)in.weight;
   double a = 0.0, by_entropy = 0.0, by_kl = 0.0, loss = 0.0, kl = row.kl;
@@ -296,26 +289,26 @@ __device__ __forceinline__ void position_done(const LossRows& rows, const LossTe
 
 // Sums of the vectors v0 .. v1 of a row by one wavefront (where the slices' records did not arrive, which never happens to calls that are
 // ordered as they have to be).
-template <int DT, bool REF> __device__ __noinline__ LossSums wave_sums(const char* row, const char* ref, int V, int v0, int v1, float c) {
+template <int DT, bool REF> __device__ __noinline__ LossSums wave_sums(const char* row, const char* ref, int V, int v0, int v1) {
   LossSums a = loss_empty();
 #pragma unroll 1
   for (int idx = v0 + (threadIdx.x & 63); idx < v1; idx += 64) {
     const uint4 x[1] = {load_vec_of<DT>(row, idx, V)}, xr[1] = {REF ? load_vec_of<DT>(ref, idx, V) : x[0]};
     loss_raise<DT, REF, 1>(a, x, xr);
-    loss_push_at<DT, REF>(a, x[0], xr[0], c);
+    loss_push_at<DT, REF>(a, x[0], xr[0]);
   }
   return loss_fold_wave<REF>(a);
 }
 
 // The elements behind the last whole vector join the first lane's sums.
-template <int DT, bool REF> __device__ __forceinline__ void push_tail(LossSums& a, const char* row, const char* ref, int V, float c) {
+template <int DT, bool REF> __device__ __forceinline__ void push_tail(LossSums& a, const char* row, const char* ref, int V) {
   uint4 x[1] = {neutral_vec<DT>()}, xr[1] = {x[0]};
   if ((threadIdx.x & 63) == 0) {
     x[0] = load_last_vec<DT>(row, V);
     xr[0] = REF ? load_last_vec<DT>(ref, V) : x[0];
   }
   loss_raise<DT, REF, 1>(a, x, xr);
-  loss_push_at<DT, REF>(a, x[0], xr[0], c);
+  loss_push_at<DT, REF>(a, x[0], xr[0]);
 }
 
 // The arrival words of the rows cut into slices: a set for each, however many there are (their last slices wait as those of few rows do: the
@@ -387,9 +380,8 @@ __global__ void __launch_bounds__(kBlock) k_loss_sums(SumsArgs args) {
   }
   if (!early) first_batch();
   ask_logit<DT>(in, row, V);
-  const float c = REF ? ref_shift<DT>(row, ref, in.x, V) : 0.f;
   LossSums a = loss_empty();
-  if (tail) push_tail<DT, REF>(a, row, ref, V, c);
+  if (tail) push_tail<DT, REF>(a, row, ref, V);
   for (int base = v0; base < v1; base += kSumsBatch * kBlock) {
     uint4 x[kSumsBatch], xr[kSumsBatch];
 #pragma unroll
@@ -404,7 +396,7 @@ __global__ void __launch_bounds__(kBlock) k_loss_sums(SumsArgs args) {
     loss_raise<DT, REF, kSumsBatch>(a, x, xr);
 #pragma unroll
     for (int k = 0; k < kSumsBatch; ++k)
-      if (base + k * kBlock < v1) loss_push_at<DT, REF>(a, x[k], REF ? xr[k] : x[k], c);
+      if (base + k * kBlock < v1) loss_push_at<DT, REF>(a, x[k], REF ? xr[k] : x[k]);
   }
   a = loss_fold_wave<REF>(a);
   if (lane == 0) sh[wave] = a;
@@ -426,10 +418,10 @@ __global__ void __launch_bounds__(kBlock) k_loss_sums(SumsArgs args) {
       a = LossSums{p.mp, p.sp, p.up, p.uq, p.mq, p.sq};
     }
     a = loss_fold_wave<REF>(a);
-    if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, vectors_of<DT>(V), c);
+    if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, vectors_of<DT>(V));
   }
   double term;
-  const LossCoef k = settle_position<REF>(late.rows, f, r, in, a, c, lane == 0, term);
+  const LossCoef k = settle_position<REF>(late.rows, f, r, in, a, lane == 0, term);
   if (lane == 0) ws.coef[r] = k;
   position_done(late.rows, f, ws, r, term);
 }
@@ -592,7 +584,6 @@ __global__ void __launch_bounds__(kBlock) k_loss_grad(LossRows rows, int pieces,
 // (which are whole there: only the slice itself would have put its gradient in their place).
 template <int W> struct JoinShared {
   LossSums sums[W];
-  float c[kWaves];
   LossCoef coef[kWaves];
   int role;             // of a slice
   uint64_t left;        // slices whose part is to be done as well
@@ -619,6 +610,7 @@ __device__ __forceinline__ bool await_result(uint64_t* at, WordWait wait, LossCo
   if (lane < kResultWords) __hip_atomic_store(at + lane, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   k.m = lane_value(word_lo(w), 0);
   k.a = lane_value(word_hi(w), 0);
+  k.c = lane_value(word_lo(w), 1);
   k.k0 = lane_value(word_hi(w), 1);
   k.k1 = lane_value(word_hi(w), 2);
   k.k2 = lane_value(word_hi(w), 3);
@@ -629,7 +621,7 @@ __device__ __forceinline__ uint64_t send_results(uint64_t* at, int S, int own, c
   const int lane = threadIdx.x & 63;
   if (lane >= S || lane == own) return 0;
   at += lane * kResultWords;
-  __hip_atomic_store(at + 1, record_word(1u, k.k0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(at + 1, record_word(bits_of(k.c) | 1u, k.k0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __hip_atomic_store(at + 2, record_word(1u, k.k1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __hip_atomic_store(at + 3, record_word(1u, k.k2), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return __hip_atomic_exchange(at, record_word(bits_of(k.m), k.a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -692,20 +684,15 @@ k_loss_join(JoinArgs args) {
   const bool on = here && position_counts(mark), on_i = RPB > 1 ? r0 + i < rows.n && position_counts(mark_i) : on;
   if (on && !early) load_row();
   if (wave == 0 && on_i && s == S - 1) ask_logit<DT>(in, row_at<DT>(rows.z, bi, ri - bi * rows.T), V);
-  float c = 0.f;
   if (on) {
-    if (REF) c = ref_shift<DT>(row, ref, x, V);
     LossSums a = loss_empty();
-    if (tail) push_tail<DT, REF>(a, row, ref, V, c);
+    if (tail) push_tail<DT, REF>(a, row, ref, V);
     loss_raise<DT, REF, NB>(a, v, REF ? q : v);
 #pragma unroll
     for (int j = 0; j < NB; ++j)
-      if (v0 + j * TR < v1) loss_push_at<DT, REF>(a, v[j], REF ? q[j] : v[j], c);
+      if (v0 + j * TR < v1) loss_push_at<DT, REF>(a, v[j], REF ? q[j] : v[j]);
     a = loss_fold_wave<REF>(a);
-    if (lane == 0) {
-      sh.sums[wave] = a;
-      sh.c[sub] = c;
-    }
+    if (lane == 0) sh.sums[wave] = a;
   }
   __syncthreads();
   x = uniform(x);
@@ -750,7 +737,7 @@ k_loss_join(JoinArgs args) {
             a = LossSums{p.mp, p.sp, p.up, p.uq, p.mq, p.sq};
           }
           a = loss_fold_wave<REF>(a);
-          if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, vectors_of<DT>(V), c);
+          if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, vectors_of<DT>(V));
         } else if (!await_result(results + s * kResultWords, f.wait, k)) {
           role = kLeaves;
         }
@@ -758,12 +745,11 @@ k_loss_join(JoinArgs args) {
       if (settles) {
         role = kSettles;
         const bool writes = on_i && (RPB > 1 ? !(lane & 1) && lane < 2 * RPB : lane == 0);
-        const LossCoef settled = settle_position<REF>(rows, f, ri, in, a, REF ? sh.c[i] : 0.f, writes, term);
+        const LossCoef settled = settle_position<REF>(rows, f, ri, in, a, writes, term);
         if (on_i) k = settled;
         else term = 0.0;
         if (RPB == 1 && S > 1) found = send_results(results, S, s, k);
       }
-      if (RPB == 1) k.c = c;
     }
     if (RPB > 1 ? !(lane & 1) && lane < 2 * RPB && r0 + i < rows.n : lane == 0) {
       sh.coef[i] = k;

@@ -137,6 +137,35 @@ def test_masks_of_any_size(am, mask, dtype):  # noqa: F811
             assert torch.isfinite(a).all() and torch.equal(a, b), (B, T, V, k)
 
 
+def _kl_spread(z, zr, o):
+    """What the terms of the KL cancel from, no token's difference by itself: the sums are about differences of the two rows' largest logits
+    (of a lane, a slice, the row).  Such a difference is z_a - y_b, y_b >= y_a, for the lane's own largest z_a: off the typical difference by |D_a| and
+    what y_b is above y_a, which is at most |D_a| + |ln p_a| + |ln max q|.  Weighted by p: 2 KL-like sums, H, and the logarithms of
+    the two rows' sums about their largest."""
+    s, sr = (torch.logsumexp(v.double(), -1) - v.double().amax(-1) for v in (z, zr))
+    return 2 * (o["p"] * o["D"].abs()).sum(-1) + o["H"] + s.abs() + sr.abs() + 1.0
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("which", ["policy", "reference"])
+@pytest.mark.parametrize("mask", [-1e4, -1e6, -1e9, -1e30])
+def test_kl_where_the_token_itself_is_masked(am, mask, which, dtype):  # noqa: F811
+    """The token's logit is a finite mask in one of the two rows: KL and gradient are those of the formula."""
+    for B, T, V in ((2, 3, 40), (3, 5, 9001), (31, 43, 1037), (2, 3, 32003), (1, 1100, 5003)):
+        c = Case(B, T, V, dtype, seed=55, masked=0.0)
+        x = torch.where(c.x == V - 1, 0, c.x + 1).to(torch.int32)                  # (next to the peak, or anywhere)
+        z, zref = c.z.clone(), (c.z.float() + 0.5 * c.n(B, T, V)).to(dtype)
+        (z if which == "policy" else zref).scatter_(-1, x.long()[..., None], mask)
+        o = R.rows(z, x, zref)
+        o["spread"] = _kl_spread(z, zref, o)
+        r = am.policy_loss(z.cuda(), x.cuda(), torch.zeros(B, T, device="cuda"), c.ws(am), ref_logits=zref.cuda(),
+                           options=am.PolicyOptions(kl_coef=1.0))
+        assert not r.status.any()
+        R.near(r.kl, o["kl"], R.tol_kl(o), "kl")
+        g, tol = R.grad(o, torch.zeros(B, T), k=torch.ones(B, T), dtype=dtype)
+        R.near(r.dlogits, g, tol, "dlogits")
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 def test_kl_of_stretches_whose_mass_is_lost(am, dtype):  # noqa: F811
     """Stretches of tokens below 2^-149 of the row's largest, of which the reference has none: they count as 0, whoever adds them up."""
