@@ -181,7 +181,7 @@ int adasd_test_logprob_grad_given_up(const adasd_rows* a, const float* dlogprob,
   return token_logprob_grad(a, dlogprob, dentropy, stream, kGivesUp);
 }
 
-int adasd_policy_loss(const adasd_rows* a, const adasd_policy_args* p, void* stream) {
+static int policy_loss(const adasd_rows* a, const adasd_policy_args* p, void* stream, WordWait wait) {
   if (!a || !p) return ADASD_ERR_INVALID_ARG;
   if (p->ref_logits && p->ref_logprob) return ADASD_ERR_INVALID_ARG;
   if (p->adv_per_seq != 0 && p->adv_per_seq != 1) return ADASD_ERR_INVALID_ARG;
@@ -196,7 +196,7 @@ int adasd_policy_loss(const adasd_rows* a, const adasd_policy_args* p, void* str
       !aligned_to(p->grad_scale, 4) || !aligned_to(p->token_loss, 4) || !aligned_to(p->kl, 4))
     return ADASD_ERR_MISALIGNED;
   LossTerm f{};
-  f.wait = kWaits;
+  f.wait = wait;
   f.kind = kPolicy;
   f.advantage = p->advantage;
   f.adv_per_seq = p->adv_per_seq;
@@ -212,6 +212,12 @@ int adasd_policy_loss(const adasd_rows* a, const adasd_policy_args* p, void* str
   f.kl = p->kl;
   return run(rows, (int)a->dt, f, ws, stream);
 }
+
+int adasd_policy_loss(const adasd_rows* a, const adasd_policy_args* p, void* stream) { return policy_loss(a, p, stream, kWaits); }
+
+// For the tests, as above.
+int adasd_test_policy_loss_unarrived(const adasd_rows* a, const adasd_policy_args* p, void* stream) { return policy_loss(a, p, stream, kNotThere); }
+int adasd_test_policy_loss_given_up(const adasd_rows* a, const adasd_policy_args* p, void* stream) { return policy_loss(a, p, stream, kGivesUp); }
 
 int adasd_preference_loss(const adasd_rows* a, const adasd_preference_args* p, void* stream) {
   if (!a || !p) return ADASD_ERR_INVALID_ARG;

@@ -813,6 +813,10 @@ k_loss_join(JoinArgs args) {
     const int other = __ffsll((long long)left) - 1, nv = vectors_of<DT>(V), u0 = min(other * chunk, nv), u1 = other == S - 1 ? nv : min(u0 + chunk, nv);
 #pragma unroll 1
     for (int idx = u0 + tid; idx < u1; idx += TR) {
+      if (zero_row(k)) {
+        zero_vec<DT>(out, idx, V);
+        continue;
+      }
       const uint4 z = load_vec_of<DT>(row, idx, V);
       emit_vec<DT, REF>(out, idx, V, x, z, REF ? load_vec_of<DT>(ref, idx, V) : z, k, ent);
     }

@@ -182,3 +182,64 @@ def test_kl_of_stretches_whose_mass_is_lost(am, dtype):  # noqa: F811
         assert torch.isfinite(got.kl).all() and torch.isfinite(got.dlogits).all() and not got.status.any()
         for name in ("loss", "token_loss", "logprob", "entropy", "kl", "dlogits"):
             assert torch.equal(getattr(got, name), getattr(want, name)), name
+
+
+def _rows_of(am, c, z, x, ws, g):  # noqa: F811
+    from test_losses import _Rows
+    rows = _Rows(z.data_ptr(), int(c.dtype == BF), c.B, c.T, c.V, z.stride(0), z.stride(1), x.data_ptr())
+    rows.workspace, rows.ws_bytes = ws.ptr, ws.bytes
+    rows.dlogits, rows.d_seq_stride, rows.d_pos_stride = g.data_ptr(), g.stride(0), g.stride(1)
+    return rows
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_zero_rows_of_slices_that_gave_up(am, dtype):  # noqa: F811
+    """A broken row with a derivative of 0 is written with zeros, also where a slice's part is done by another workgroup."""
+    import ctypes
+    lib = am.load_library()
+    for B, T, V in ((1, 2, 128256), (3, 5, 32003), (1, 700, 20011)):
+        c = Case(B, T, V, dtype, seed=57, masked=0.0)
+        z, x, ws = c.z.clone(), c.x.cuda(), c.ws(am)
+        z[:, 0::2, V // 3] = math.nan
+        z = z.cuda()
+        a = torch.ones(B, T, device="cuda")
+        a[:, 0::2] = 0.0
+        g = torch.full_like(z, 9.0)
+        rows = _rows_of(am, c, z, x, ws, g)
+        s = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        assert lib.adasd_test_logprob_grad_given_up(ctypes.byref(rows), ctypes.c_void_p(a.data_ptr()), None, s) == 0
+        torch.cuda.synchronize()
+        assert not g[:, 0::2].any() and torch.isfinite(g).all()
+
+
+@pytest.mark.parametrize("how", ["unarrived", "given_up"])
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_policy_loss_whose_records_are_not_waited_for(am, how, dtype):  # noqa: F811
+    """A reference's rows and an entropy bonus, where no slice waits for the others' sums, or all count as not there; the gradient
+    in the logits' place too (but where records count as not there: they are formed from the logits again)."""
+    import ctypes
+    from test_losses import _PolicyArgs
+    lib = am.load_library()
+    for B, T, V in ((1, 2, 128256), (3, 5, 32003), (1, 700, 20011)):
+        c = Case(B, T, V, dtype, seed=64)
+        zref = (c.z.float() + 0.5 * c.n(B, T, V)).to(dtype)
+        adv, old = c.n(B, T), c.old()
+        e = R.policy(c.z, c.x, adv, weight=c.w, old=old, zref=zref, kl_coef=0.1, ent=0.01)
+        x, ws, q = c.x.cuda(), c.ws(am), zref.cuda()
+        d = [v.cuda() for v in (adv, old, c.w)]
+        f = getattr(lib, f"adasd_test_policy_loss_{how}")
+        for in_place in (False, True) if how == "given_up" else (False,):
+            z = c.z.cuda()
+            g = z if in_place else torch.full_like(z, 9.0)
+            out = torch.full((2 * B * T + 1,), 9.0, device="cuda")
+            rows = _rows_of(am, c, z, x, ws, g)
+            rows.weight = d[2].data_ptr()
+            p = _PolicyArgs(d[0].data_ptr(), 0, d[1].data_ptr(), None, q.data_ptr(), q.stride(0), q.stride(1), None, 0.2, 0.2, 0.1, 0.01,
+                            out.data_ptr(), out[1:].data_ptr(), out[1 + B * T:].data_ptr())
+            s = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+            assert f(ctypes.byref(rows), ctypes.byref(p), s) == 0
+            torch.cuda.synchronize()
+            R.near(out[0], e["loss"], e["loss_tol"], "loss")
+            R.near(out[1:1 + B * T].view(B, T), e["term"], e["term_tol"], "token_loss")
+            R.near(out[1 + B * T:].view(B, T), e["kl"], e["kl_tol"], "kl")
+            R.near(g, e["g"], e["g_tol"], "dlogits")
