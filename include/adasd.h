@@ -380,7 +380,8 @@ int adasd_update_thresholds(const adasd_state *st /* host */, int k_max, const i
  *   need not be numbers, or a token of the vocabulary), its results are 0, and its row of dlogits is written with zeros;
  *   status[b,t]    = ADASD_ST_BAD_TOKEN (token outside [0,V): log-probability NaN), ADASD_ST_NONFINITE (a NaN in the row, no
  *                    finite logit, or a largest one beyond 2^26 in size: results NaN; a reference's row likewise), or 0.  A
- *                    gradient row that depends on a NaN is NaN.
+ *                    gradient row that depends on a NaN is NaN, one that depends on the log-probability of a token outside
+ *                    the vocabulary too.
  * Logits of -inf, or of the type's lowest value beside ordinary ones, are tokens without mass: gradient 0 there.
  * Gradients have the type of the logits (formed in 32 bits, rounded once).  dlogits may be the logits' own memory (same pointer and
  * strides: the gradient takes their place); any other address range that overlaps that of logits the call reads is refused.

@@ -477,7 +477,8 @@ def token_logprob_grad(logits: torch.Tensor, tokens: torch.Tensor, workspace: Lo
                        dentropy: Optional[torch.Tensor] = None, active: Optional[torch.Tensor] = None,
                        dlogits: Optional[torch.Tensor] = None) -> torch.Tensor:
     """adasd_token_logprob_grad: the gradient of a loss by the logits, given its derivatives by token_logprob's log-probabilities and
-    entropies.  dlogits may be `logits` itself.  Pass it on with ``logits.backward(dlogits)``."""
+    entropies.  dlogits may be `logits` itself.  Pass it on with ``logits.backward(dlogits)``.  Rows of tokens outside the
+    vocabulary are NaN, unless they are not active or their derivative is 0."""
     return (_native or _connect()).token_logprob_grad(logits, tokens, workspace, dlogprob, dentropy, active, dlogits)
 
 

@@ -67,7 +67,7 @@ __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const 
   double a = 0.0, by_entropy = 0.0, by_kl = 0.0, loss = 0.0, kl = row.kl;
   term = 0.0;
   if (f.kind == kLogprob) {
-    a = (double)in.a;
+    a = known || in.a == 0.f ? (double)in.a : lp;           // (a gradient that hangs on a log-probability that is none)
     by_entropy = (double)in.h;
   } else if (f.kind == kPolicy) {
     // one exponential for both ratios: the old policy's in the even lanes, the reference's in the odd ones

@@ -243,3 +243,21 @@ def test_policy_loss_whose_records_are_not_waited_for(am, how, dtype):  # noqa: 
             R.near(out[1:1 + B * T].view(B, T), e["term"], e["term_tol"], "token_loss")
             R.near(out[1 + B * T:].view(B, T), e["kl"], e["kl_tol"], "kl")
             R.near(g, e["g"], e["g_tol"], "dlogits")
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_gradient_of_a_token_outside_the_vocabulary(am, dtype):  # noqa: F811
+    """Its log-probability is NaN, and so is a gradient row that hangs on it; the entropy's gradient needs no token."""
+    for B, T, V in ((1, 6, 40), (2, 3, 32003), (31, 43, 1037)):
+        c = Case(B, T, V, dtype, seed=58, masked=0.0)
+        x = c.x.clone()
+        x[0, 1], x[0, 2] = -100, V
+        a, h = c.n(B, T), c.n(B, T)
+        a[0, 2] = 0.0
+        o = R.rows(c.z, c.x)
+        for dH in (None, h):
+            g = am.token_logprob_grad(c.z.cuda(), x.cuda(), c.ws(am), a.cuda(), cu(dH))
+            assert torch.isnan(g[0, 1]).all()
+            want, tol = R.grad(o, a, dH, dtype=dtype)
+            g[0, 1] = want[0, 1].to(g)
+            R.near(g, want, tol, "dlogits")
