@@ -425,7 +425,7 @@ int adasd_token_logprob_grad(const adasd_rows *rows /* host */, const float *dlo
 /*
  * Clipped policy loss.  With r = exp(logprob - old_logprob) and the advantage A of the position,
  *   term = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A) + kl_coef KL - entropy_coef H,   loss = sum over (b,t) of weight term,
- *   KL   = exp(d) - 1 - d with d = ref_logprob - logprob (the sampled token's estimate), or, with ref_logits,
+ *   KL   = exp(d) - 1 - d with d = ref_logprob - logprob (the sampled token's estimate; +inf at d = +-inf), or, with ref_logits,
  *          sum_j p_j (ln p_j - ln q_j) over the vocabulary (+inf where q_j = 0 < p_j; such a row's gradient is NaN; a p_j below
  *          2^-149 of the row's largest is 0), or 0 without either.  (Both given: ADASD_ERR_INVALID_ARG.)
  * Where A is 0 the first part is 0 whatever r is; a coefficient of 0 leaves its part out.  dlogits is the derivative of

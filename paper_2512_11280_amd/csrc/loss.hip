@@ -81,7 +81,8 @@ __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const 
       a = clipped ? 0.0 : -free;
     }
     if (f.ref_logprob) {
-      kl = grown_ref - ((double)in.ref - lp);
+      const double d = (double)in.ref - lp;
+      kl = d < INFINITY ? grown_ref - d : d;
       if (f.kl_coef != 0.f) a -= (double)f.kl_coef * grown_ref;
     }
     if (f.kl_coef != 0.f) loss += (double)f.kl_coef * kl;

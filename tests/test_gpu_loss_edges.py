@@ -261,3 +261,19 @@ def test_gradient_of_a_token_outside_the_vocabulary(am, dtype):  # noqa: F811
             want, tol = R.grad(o, a, dH, dtype=dtype)
             g[0, 1] = want[0, 1].to(g)
             R.near(g, want, tol, "dlogits")
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_sampled_kl_of_tokens_without_mass(am, dtype):  # noqa: F811
+    """exp(d) - 1 - d is +inf at both ends: a token without mass in the row (d = +inf), or in the reference (d = -inf)."""
+    for B, T, V in ((2, 3, 40), (2, 3, 32003), (31, 43, 1037)):
+        c = Case(B, T, V, dtype, seed=59, masked=0.0)
+        z, ref = c.z.clone(), c.lp.float().clone()
+        z[0, 0, int(c.x[0, 0])] = -INF
+        ref[0, 1] = -INF
+        one = torch.ones(B, T, device="cuda")
+        o = am.policy_loss(z.cuda(), c.x.cuda(), one, c.ws(am), ref_logprob=ref.cuda(), old_logprob=c.old().cuda(),
+                           options=am.PolicyOptions(kl_coef=0.1))
+        assert o.kl[0, 0].item() == INF and o.kl[0, 1].item() == INF and torch.isfinite(o.kl.cpu().view(-1)[2:]).all()
+        assert o.token_loss[0, 0].item() == INF and o.token_loss[0, 1].item() == INF and o.loss.item() == INF
+        assert torch.isfinite(o.dlogits[0, 1]).all() and not torch.isfinite(o.dlogits[0, 0, int(c.x[0, 0])]).item()
