@@ -87,10 +87,11 @@ __device__ __forceinline__ double log1p_fine(double x) {
   p = fma(p, g, 1.0 / 3);
   return 2.0 * fma(p * g, f, f);
 }
-// e^d - 1 to about 1e-14 relative, whatever the size of d: e^d = 2^k e^r, |r| <= ln 2 / 2, and the series of e^r - 1.
-__device__ __forceinline__ double expm1_fine(double d) {
-  const double k = rint(fmin(fmax(d, -800.0), 800.0) * 1.44269504088896340736);
-  double r = fma(-k, 0x1.62e42fee00000p-1, d);                     // (ln 2 in two parts, the first with zeros at its end)
+// e^d = 2^k (1 + p): k, and p = e^r - 1 by its series, r = d - k ln 2, |r| <= ln 2 / 2 (ln 2 in two parts, the first with zeros at its end, so that
+// its product with k is exact: Cody and Waite's reduction).  About 1e-14 relative.
+__device__ __forceinline__ double exp_part(double d, double& k) {
+  k = rint(fmin(fmax(d, -800.0), 800.0) * 1.44269504088896340736);
+  double r = fma(-k, 0x1.62e42fee00000p-1, d);
   r = fma(-k, 0x1.a39ef35793c76p-33, r);
   double p = 1.0 / 39916800;
   p = fma(p, r, 1.0 / 3628800);
@@ -102,9 +103,19 @@ __device__ __forceinline__ double expm1_fine(double d) {
   p = fma(p, r, 1.0 / 24);
   p = fma(p, r, 1.0 / 6);
   p = fma(p, r, 0.5);
-  p = fma(p * r, r, r);
-  const double v = k == 0.0 ? p : ldexp(p + 1.0, (int)k) - 1.0;
+  return fma(p * r, r, r);
+}
+// e^d - 1, whatever the size of d.
+__device__ __forceinline__ double expm1_fine(double d) {
+  double k;
+  const double p = exp_part(d, k), v = k == 0.0 ? p : ldexp(p + 1.0, (int)k) - 1.0;
   return d > 709.0 ? (double)INFINITY : d < -745.0 ? -1.0 : v;     // (NaN: neither)
+}
+// e^d, d <= 0.
+__device__ __forceinline__ double exp_fine(double d) {
+  double k;
+  const double v = ldexp(exp_part(d, k) + 1.0, (int)k);
+  return d < -745.0 ? 0.0 : v;
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -236,7 +236,7 @@ __device__ __forceinline__ void settle_pair(const LossTerm& f, const LossWorkspa
       slope = m < 1.0 ? -beta : 0.0;
     } else {
       // ln(1 + e^(-m)) = max(-m, 0) + ln(1 + e^-|m|), and the same of m
-      const double E = expm1_fine(-fabs(m)) + 1.0, tail = log1p_fine(E), small = E / (1.0 + E), large = 1.0 / (1.0 + E);
+      const double E = exp_fine(-fabs(m)), tail = log1p_fine(E), small = E / (1.0 + E), large = 1.0 / (1.0 + E);
       // (a part with factor 0 is left out: it may be infinite)
       loss = tail + (e < 1.0 ? (1.0 - e) * fmax(-m, 0.0) : 0.0) + (e > 0.0 ? e * fmax(m, 0.0) : 0.0);
       slope = beta * (e * (m >= 0.0 ? large : small) - (1.0 - e) * (m >= 0.0 ? small : large));

@@ -277,3 +277,27 @@ def test_sampled_kl_of_tokens_without_mass(am, dtype):  # noqa: F811
         assert o.kl[0, 0].item() == INF and o.kl[0, 1].item() == INF and torch.isfinite(o.kl.cpu().view(-1)[2:]).all()
         assert o.token_loss[0, 0].item() == INF and o.token_loss[0, 1].item() == INF and o.loss.item() == INF
         assert torch.isfinite(o.dlogits[0, 1]).all() and not torch.isfinite(o.dlogits[0, 0, int(c.x[0, 0])]).item()
+
+
+@pytest.mark.parametrize("margin", [0.0, 3.0, 17.0, 30.0, 34.0, 38.0, 60.0, 80.0])
+def test_logistic_loss_of_large_margins(am, margin):  # noqa: F811
+    """Loss and gradients of a pair that is far apart are small, and right to the last digits: float logits of two tokens, a margin set by the
+    reference's log-probabilities.  m is formed in 64 bits from a float log-probability's sums (r of loss_ref for two scores, beta 1) and e^-m is off by
+    that error relatively; loss and gradient are rounded twice more (4 steps of float are allowed)."""
+    V = 8
+    z = torch.randn(2, 1, V, generator=torch.Generator().manual_seed(60))
+    x = torch.tensor([[1], [2]], dtype=torch.int32)
+    lp = R.rows(z, x)["lp"]
+    for sign in (1.0, -1.0):
+        ref = (lp - torch.tensor([[sign * margin], [0.0]])).float()
+        o = am.preference_loss(z.cuda(), x.cuda(), am.LossWorkspace(2, 1, V, F), ref_logprob=ref.cuda(), options=am.PreferenceOptions(beta=1.0))
+        e = R.rows(z, x)
+        m = (e["lp"] - ref.double())[0, 0] - (e["lp"] - ref.double())[1, 0]
+        loss, slope = torch.log1p(torch.exp(-m.abs())) + (-m).clamp_min(0.0), -1.0 / (1.0 + torch.exp(m))
+        rel = 2 * e["r"] + 4 * R.H24
+        assert abs(o.pair_loss.item() - loss.item()) <= rel * loss.item()
+        p = e["p"][:, 0]
+        g = torch.stack([slope * ((torch.arange(V) == 1).double() - p[0]), -slope * ((torch.arange(V) == 2).double() - p[1])])
+        # (1 - p of the token: both parts are rounded)
+        tol = slope.abs() * (rel + e["r"] + 4 * R.H24) * (p + torch.stack([(torch.arange(V) == k).double() for k in (1, 2)]))
+        R.near(o.dlogits[:, 0], g, tol, "dlogits")
