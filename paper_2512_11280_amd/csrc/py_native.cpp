@@ -394,6 +394,7 @@ struct RowsCall {
   int64_t shape[2];
   int dims;
   void* stream;
+  c10::Allocator* allocator;
   c10::hip::OptionalHIPGuard guard;       // the calls run on the logits' device, whatever the current one is
 
   RowsCall(PyObject* logits, PyObject* tokens, PyObject* workspace, bool only_sequences) {
@@ -415,6 +416,7 @@ struct RowsCall {
     rows.tokens = (const int32_t*)input(tokens, at::kInt, "tokens");
     Ref buf(workspace, N->buf);
     if (tensor(buf.o, "workspace.buf").device() != z->device()) fail(PyExc_ValueError, "workspace must be on the logits' device");
+    allocator = THPVariable_Unpack(buf.o).storage().allocator();
     rows.workspace = (void*)int_attr(workspace, N->ptr);
     rows.ws_bytes = int_attr(workspace, N->bytes);
     guard.set_index(z->get_device());
@@ -439,6 +441,18 @@ struct RowsCall {
   void* input(PyObject* o, at::ScalarType type, const char* name) const { return input(o, type, name, shape, dims); }
   void* maybe(PyObject* o, at::ScalarType type, const char* name) const { return given(o) ? input(o, type, name) : nullptr; }
   const float* one(PyObject* o, int64_t n, const char* name) const { return given(o) ? (const float*)input(o, at::kFloat, name, &n, 1) : nullptr; }
+
+  // A new result, as at::empty makes one, from the workspace's allocator (without the dispatcher's part: calls of one token are short).
+  at::Tensor result(at::IntArrayRef sizes, at::ScalarType t) const {
+    if (!allocator) return at::empty(sizes, z->options().dtype(t));
+    int64_t bytes = 4;                         // (every result has elements of 4 bytes)
+    for (int64_t d : sizes) bytes *= d;
+    auto storage = c10::make_intrusive<c10::StorageImpl>(c10::StorageImpl::use_byte_size_t(), bytes, allocator->allocate(bytes), allocator, true);
+    auto made = c10::make_intrusive<c10::TensorImpl>(c10::Storage(std::move(storage)), c10::DispatchKeySet(c10::DispatchKey::CUDA),
+                                                     c10::scalarTypeToTypeMeta(t));
+    made->set_sizes_contiguous(sizes);
+    return at::Tensor(std::move(made));
+  }
 
   // The gradient: the caller's tensor (any strides with a contiguous vocabulary), or a new one.  New reference.
   PyObject* gradient(PyObject* o) {
@@ -466,14 +480,11 @@ struct RowsCall {
   }
 };
 
-// Results to be handed over together: the caller's tensors, or parts of one allocation for all that are new (a tensor of its own takes
-// 0.7 us each, more than the smallest call has to spare; a part that is kept keeps the others' memory, 20 bytes a position).
+// Results to be handed over together: the caller's tensors, or new ones, each with a storage of its own (results are kept and saved one by
+// one: parts of one allocation would keep and save all of it, and torch does not save parts of different types).
 template <int M> struct Results {
   const RowsCall& c;
   PyObject* o[M] = {};
-  int64_t elements[M], at[M], bytes = 0;
-  at::ScalarType type[M];
-  at::SmallVector<int64_t, 2> size[M];
   int n = 0;
   explicit Results(const RowsCall& call) : c(call) {}
   ~Results() {
@@ -484,34 +495,12 @@ template <int M> struct Results {
     o[n] = p;
     return n++;
   }
-  int make(at::IntArrayRef sizes, at::ScalarType t) {
-    size[n].assign(sizes.begin(), sizes.end());
-    type[n] = t;
-    int64_t count = 1;
-    for (int64_t d : sizes) count *= d;
-    at[n] = bytes;
-    bytes += (4 * count + 63) / 64 * 64;       // (every result has elements of 4 bytes)
-    return n++;
-  }
+  int make(at::IntArrayRef sizes, at::ScalarType t) { return add(RowsCall::wrap(c.result(sizes, t))); }
   int take(PyObject* given_one, at::ScalarType t, const char* name) {      // the caller's, in the shape of the tokens, or a new one
     if (!given(given_one)) return make(at::IntArrayRef(c.shape, c.dims), t);
     c.input(given_one, t, name);
     Py_INCREF(given_one);
     return add(given_one);
-  }
-  void allocate() {
-    bool missing = false;
-    for (int i = 0; i < n; ++i) missing = missing || !o[i];
-    if (!missing) return;
-    const at::Tensor all = at::empty({bytes / 4}, c.z->options().dtype(at::kFloat));
-    for (int i = 0; i < n; ++i) {
-      if (o[i]) continue;
-      auto part = c10::make_intrusive<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(all.storage()), all.key_set(),
-                                                       c10::scalarTypeToTypeMeta(type[i]));
-      part->set_sizes_contiguous(size[i]);
-      part->set_storage_offset(at[i] / 4);
-      o[i] = RowsCall::wrap(at::Tensor(std::move(part)));
-    }
   }
   template <class T> T* ptr(int i) const { return (T*)THPVariable_Unpack(o[i]).data_ptr(); }
   PyObject* tuple() {
@@ -553,7 +542,6 @@ PyObject* py_token_logprob(PyObject*, PyObject* const* args, Py_ssize_t nargs, P
     out.take(a[4], at::kFloat, "logprob_out");
     out.take(a[5], at::kFloat, "entropy_out");
     out.take(a[6], at::kInt, "status_out");
-    out.allocate();
     c.rows.logprob = out.ptr<float>(0);
     c.rows.entropy = out.ptr<float>(1);
     c.rows.status = out.ptr<uint32_t>(2);
@@ -616,7 +604,6 @@ PyObject* py_policy_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyO
     out.make({}, at::kFloat);
     for (int i = 1; i < 5; ++i) out.make(size, at::kFloat);
     out.make(size, at::kInt);
-    out.allocate();
     p.loss = out.ptr<float>(0);
     p.token_loss = out.ptr<float>(1);
     c.rows.logprob = out.ptr<float>(2);
@@ -660,7 +647,6 @@ PyObject* py_preference_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs,
     out.make(at::IntArrayRef(c.shape, 1), at::kFloat);
     out.make(at::IntArrayRef(c.shape, 2), at::kFloat);
     out.make(at::IntArrayRef(c.shape, 2), at::kInt);
-    out.allocate();
     p.loss = out.ptr<float>(0);
     p.pair_loss = out.ptr<float>(1);
     p.pair_margin = out.ptr<float>(2);

@@ -301,3 +301,24 @@ def test_logistic_loss_of_large_margins(am, margin):  # noqa: F811
         # (1 - p of the token: both parts are rounded)
         tol = slope.abs() * (rel + e["r"] + 4 * R.H24) * (p + torch.stack([(torch.arange(V) == k).double() for k in (1, 2)]))
         R.near(o.dlogits[:, 0], g, tol, "dlogits")
+
+
+def test_results_are_tensors_of_their_own(am):  # noqa: F811
+    """Each result has its storage: it can be kept, saved and written to by itself."""
+    import io
+    c = Case(4, 3, 40, F, seed=61)
+    z, x, ws, one = c.z.cuda(), c.x.cuda(), c.ws(am), torch.ones(4, 3, device="cuda")
+    results = [am.token_logprob(z, x, ws), list(vars(am.policy_loss(z, x, one, ws)).values()), list(vars(am.preference_loss(z, x, ws)).values())]
+    for r in results:
+        assert len({t.untyped_storage().data_ptr() for t in r}) == len(r)
+        for t in r:
+            assert t.untyped_storage().nbytes() == t.numel() * t.element_size() and t.storage_offset() == 0 and t.is_contiguous()
+        f = io.BytesIO()
+        torch.save(list(r), f)
+        f.seek(0)
+        assert all(torch.equal(a.cpu(), b) for a, b in zip(r, torch.load(f, map_location="cpu", weights_only=True)))
+    with torch.inference_mode():
+        lp = am.token_logprob(z, x, ws)[0]
+        assert lp.is_inference()
+    empty = am.token_logprob(torch.empty(0, 40, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"), ws)
+    assert all(t.shape == (0,) for t in empty)
