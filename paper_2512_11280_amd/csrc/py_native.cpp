@@ -395,6 +395,8 @@ struct RowsCall {
   int dims;
   void* stream;
   c10::Allocator* allocator;
+  const at::Tensor* written[4];           // (the gradient, or the three results of a log-probability call)
+  int n_written = 0;
   c10::hip::OptionalHIPGuard guard;       // the calls run on the logits' device, whatever the current one is
 
   RowsCall(PyObject* logits, PyObject* tokens, PyObject* workspace, bool only_sequences) {
@@ -442,6 +444,14 @@ struct RowsCall {
   void* maybe(PyObject* o, at::ScalarType type, const char* name) const { return given(o) ? input(o, type, name) : nullptr; }
   const float* one(PyObject* o, int64_t n, const char* name) const { return given(o) ? (const float*)input(o, at::kFloat, name, &n, 1) : nullptr; }
 
+  // The caller's tensors that the call writes to: torch learns of it as of its own writes in place (a backward pass that needs what was there
+  // then says so).  Inference tensors keep no count.
+  void written_to(const at::Tensor& t) { written[n_written++] = &t; }
+  void enqueued() const {
+    for (int i = 0; i < n_written; ++i)
+      if (!written[i]->is_inference()) written[i]->unsafeGetTensorImpl()->bump_version();
+  }
+
   // A new result, as at::empty makes one, from the workspace's allocator (without the dispatcher's part: calls of one token are short).
   at::Tensor result(at::IntArrayRef sizes, at::ScalarType t) const {
     if (!allocator) return at::empty(sizes, z->options().dtype(t));
@@ -461,6 +471,7 @@ struct RowsCall {
       if (g.device() != z->device() || g.scalar_type() != z->scalar_type() || g.sizes() != z->sizes() || (rows.V > 1 && g.stride(dims) != 1))
         fail(PyExc_ValueError, "dlogits must have the shape, type and device of the logits and a contiguous vocabulary");
       place(g);
+      written_to(g);
       Py_INCREF(o);
       return o;
     }
@@ -483,10 +494,10 @@ struct RowsCall {
 // Results to be handed over together: the caller's tensors, or new ones, each with a storage of its own (results are kept and saved one by
 // one: parts of one allocation would keep and save all of it, and torch does not save parts of different types).
 template <int M> struct Results {
-  const RowsCall& c;
+  RowsCall& c;
   PyObject* o[M] = {};
   int n = 0;
-  explicit Results(const RowsCall& call) : c(call) {}
+  explicit Results(RowsCall& call) : c(call) {}
   ~Results() {
     for (int i = 0; i < n; ++i) Py_XDECREF(o[i]);
   }
@@ -499,6 +510,7 @@ template <int M> struct Results {
   int take(PyObject* given_one, at::ScalarType t, const char* name) {      // the caller's, in the shape of the tokens, or a new one
     if (!given(given_one)) return make(at::IntArrayRef(c.shape, c.dims), t);
     c.input(given_one, t, name);
+    c.written_to(THPVariable_Unpack(given_one));
     Py_INCREF(given_one);
     return add(given_one);
   }
@@ -516,12 +528,13 @@ template <int M> struct Results {
     return r;
   }
 };
-template <class F> void enqueue(const char* where, F f) {
+template <class F> void enqueue(const char* where, const RowsCall& c, F f) {
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = f();
   Py_END_ALLOW_THREADS
   check(rc, where);
+  c.enqueued();
 }
 bool truth(PyObject* o, bool fallback) {
   if (!o) return fallback;
@@ -545,7 +558,7 @@ PyObject* py_token_logprob(PyObject*, PyObject* const* args, Py_ssize_t nargs, P
     c.rows.logprob = out.ptr<float>(0);
     c.rows.entropy = out.ptr<float>(1);
     c.rows.status = out.ptr<uint32_t>(2);
-    enqueue("adasd_token_logprob", [&] { return g_abi.token_logprob(&c.rows, c.stream); });
+    enqueue("adasd_token_logprob", c, [&] { return g_abi.token_logprob(&c.rows, c.stream); });
     return out.tuple();
   });
 }
@@ -562,7 +575,7 @@ PyObject* py_token_logprob_grad(PyObject*, PyObject* const* args, Py_ssize_t nar
     c.rows.active = (const uint8_t*)c.maybe(a[5], at::kByte, "active");
     Results<1> out(c);
     out.add(c.gradient(a[6]));
-    enqueue("adasd_token_logprob_grad", [&] { return g_abi.token_logprob_grad(&c.rows, dlp, dent, c.stream); });
+    enqueue("adasd_token_logprob_grad", c, [&] { return g_abi.token_logprob_grad(&c.rows, dlp, dent, c.stream); });
     out.n = 0;
     return out.o[0];
   });
@@ -611,7 +624,7 @@ PyObject* py_policy_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyO
     p.kl = out.ptr<float>(4);
     c.rows.status = out.ptr<uint32_t>(5);
     out.add(truth(a[10], true) ? c.gradient(a[11]) : Py_NewRef(Py_None));
-    enqueue("adasd_policy_loss", [&] { return g_abi.policy_loss(&c.rows, &p, c.stream); });
+    enqueue("adasd_policy_loss", c, [&] { return g_abi.policy_loss(&c.rows, &p, c.stream); });
     return out.call(g_policy_result);
   });
 }
@@ -654,7 +667,7 @@ PyObject* py_preference_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs,
     c.rows.logprob = out.ptr<float>(4);
     c.rows.status = out.ptr<uint32_t>(5);
     out.add(truth(a[8], true) ? c.gradient(a[9]) : Py_NewRef(Py_None));
-    enqueue("adasd_preference_loss", [&] { return g_abi.preference_loss(&c.rows, &p, c.stream); });
+    enqueue("adasd_preference_loss", c, [&] { return g_abi.preference_loss(&c.rows, &p, c.stream); });
     return out.call(g_preference_result);
   });
 }

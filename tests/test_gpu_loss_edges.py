@@ -322,3 +322,31 @@ def test_results_are_tensors_of_their_own(am):  # noqa: F811
         assert lp.is_inference()
     empty = am.token_logprob(torch.empty(0, 40, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"), ws)
     assert all(t.shape == (0,) for t in empty)
+
+
+def test_tensors_written_to_are_known_to_torch(am):  # noqa: F811
+    """A gradient in the place of logits that torch has saved for a backward pass is noticed there, as every write in place is."""
+    c = Case(2, 3, 40, F, seed=62)
+    ws, x, one = c.ws(am), c.x.cuda(), torch.ones(2, 3, device="cuda")
+    h = c.z.cuda().requires_grad_(True)
+    for call in (lambda v: am.token_logprob_grad(v, x, ws, one, dlogits=v), lambda v: am.policy_loss(v, x, one, ws, dlogits=v),
+                 lambda v: am.preference_loss(v, x, ws, dlogits=v)):
+        z = torch.tanh(h)                                    # (tanh's backward needs its result)
+        before = z._version
+        call(z)
+        assert z._version == before + 1
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            z.sum().backward()
+        z = h * 3.0                                          # (this one's does not)
+        call(z)
+        z.backward(z.detach())
+    given = [torch.empty(2, 3, device="cuda"), torch.empty(2, 3, device="cuda"), torch.empty(2, 3, dtype=torch.int32, device="cuda")]
+    z = c.z.cuda()
+    am.token_logprob(z, x, ws, None, *given)
+    assert [t._version for t in given] == [1, 1, 1] and z._version == 0
+    am.policy_loss(z, x, one, ws)
+    assert z._version == 0
+    with torch.inference_mode():
+        y = c.z.cuda()
+        am.policy_loss(y, x, one, ws, dlogits=y)
+    am.policy_loss(y, x, one, ws, dlogits=y)                 # (an inference tensor has no version)
