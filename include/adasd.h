@@ -410,7 +410,8 @@ typedef struct {
 } adasd_rows;
 
 /* Scratch of the calls below for B x T positions over V (serves any smaller B*T; with a longer V, or logits of another type, the
- * same results may take longer).  Calls that share one must be ordered on one stream. */
+ * same results may take longer).  Calls that share one must be ordered on one stream.  It is laid out differently from the workspace
+ * of the verification and drafting calls: the two must not share memory. */
 int adasd_loss_workspace_bytes(int B, int T, int V, adasd_dtype dt, size_t *bytes /* host */);
 
 /* logprob, entropy and status of every active position (dlogits is not touched).  One read of the logits. */

@@ -122,7 +122,7 @@ def _connect():
     native.connect(AdasdError, alloc_verify_result,
                    *(C.cast(getattr(L, "adasd_" + f), C.c_void_p).value
                      for f in ("draft_entropy", "draft_step", "verify", "verify_noalloc")))
-    native.connect_losses(PolicyResult, PreferenceResult,
+    native.connect_losses(PolicyResult, PreferenceResult, LossWorkspace,
                           *(C.cast(getattr(L, "adasd_" + f), C.c_void_p).value
                             for f in ("token_logprob", "token_logprob_grad", "policy_loss", "preference_loss")))
     _native = native
@@ -295,6 +295,13 @@ class Shard:
         return _Shard(self.n_shards, self.shard, self.V_total, self.col_begin)
 
 
+def _scratch(workspace):
+    """Address and size of the workspace of a call that is not one of the losses' (theirs is laid out differently)."""
+    if isinstance(workspace, LossWorkspace):
+        raise TypeError("workspace must be a Workspace (a LossWorkspace is laid out differently)")
+    return workspace.ptr, workspace.bytes
+
+
 def _local_args(target_local, draft_local, draft_tokens, workspace, draft_len, seed=0, seq_id=None, rounds=None,
                 round0=0, next_token=None, status=None) -> _VerifyArgs:
     """adasd_verify_args of a local (column slice) call: logits and strides of the slice, no outputs."""
@@ -312,7 +319,7 @@ def _local_args(target_local, draft_local, draft_tokens, workspace, draft_len, s
         draft_local.stride(0) if K > 0 else V, draft_local.stride(1) if K > 0 else V,
         draft_tokens.data_ptr(), _p(draft_len), None, seed & 0xFFFFFFFFFFFFFFFF, _p(seq_id), _p(rounds),
         round0 & 0xFFFFFFFF, None, _p(next_token), None, None, None, None, None, _p(status),
-        workspace.ptr, workspace.bytes)
+        *_scratch(workspace))
 
 
 def verify_shard_stats(target_local, draft_local, draft_tokens, workspace: Workspace, shard: Shard,
@@ -355,7 +362,7 @@ def _meta_args(B, k, dtype, draft_tokens, workspace, shard, out, state=None, dra
         seed & 0xFFFFFFFFFFFFFFFF, _p(seq_id), _p(rounds), round0 & 0xFFFFFFFF,
         out.n_accept.data_ptr(), out.next_token.data_ptr(), out.H_p.data_ptr(), out.H_q.data_ptr(),
         out.d_js.data_ptr(), out.p_accept.data_ptr(), out.accept_mask.data_ptr(),
-        out.status.data_ptr(), workspace.ptr, workspace.bytes)
+        out.status.data_ptr(), *_scratch(workspace))
     a._keep = st            # the struct only holds a pointer to it
     return a
 
@@ -451,7 +458,8 @@ def update_thresholds(state: State, k_max: int, n_accept: torch.Tensor, H_q: tor
 
 class LossWorkspace:
     """Device scratch of token_logprob, token_logprob_grad, policy_loss and preference_loss for B x T positions (or fewer) over a
-    vocabulary of V (allocated through torch).  Calls that share one must be ordered on one stream."""
+    vocabulary of V (allocated through torch).  Calls that share one must be ordered on one stream.  Not for the verification and drafting
+    calls, whose Workspace is laid out differently; either kind refuses the other's."""
 
     def __init__(self, B: int, T: int, V: int, dtype: torch.dtype, device="cuda"):
         n = C.c_size_t()

@@ -33,6 +33,7 @@ struct Abi {
 PyObject* g_error = nullptr;         // AdasdError(code, where)
 PyObject* g_alloc_result = nullptr;  // alloc_verify_result(B, K, device)
 PyObject* g_policy_result = nullptr, *g_preference_result = nullptr;   // PolicyResult, PreferenceResult
+PyObject* g_loss_workspace = nullptr;   // LossWorkspace
 
 struct Fail {};                      // a Python exception is set
 
@@ -146,9 +147,35 @@ adasd_dtype logits_type(PyObject* o) {
   }
   throw Fail{};
 }
-void* stream() { return (void*)c10::hip::getCurrentHIPStream().stream(); }
-
 PyObject* intern(const char* s) { return PyUnicode_InternFromString(s); }
+
+struct Names {
+  PyObject *ptr = intern("ptr"), *bytes = intern("bytes"), *B = intern("B"), *cap = intern("cap"), *T_G = intern("T_G"),
+           *ent_sum = intern("ent_sum"), *ent_cnt = intern("ent_cnt"), *LA = intern("LA"), *LR = intern("LR"),
+           *nA = intern("nA"), *nR = intern("nR"), *mom = intern("mom"), *n_accept = intern("n_accept"),
+           *next_token = intern("next_token"), *H_p = intern("H_p"), *H_q = intern("H_q"), *d_js = intern("d_js"),
+           *p_accept = intern("p_accept"), *accept_mask = intern("accept_mask"), *status = intern("status"),
+           *base_test = intern("base_test"), *reject_rule = intern("reject_rule"), *kde_min_n = intern("kde_min_n"),
+           *bw_rule = intern("bw_rule"), *relaxed_off = intern("relaxed_off"), *d_eps = intern("d_eps"),
+           *stats_path = intern("stats_path"), *apply_update = intern("apply_update"), *list_update = intern("list_update"),
+           *wait_polls = intern("wait_polls"), *buf = intern("buf"), *clip_low = intern("clip_low"), *clip_high = intern("clip_high"),
+           *kl_coef = intern("kl_coef"), *entropy_coef = intern("entropy_coef"), *kind = intern("kind"), *beta = intern("beta"),
+           *margin = intern("margin"), *label_smoothing = intern("label_smoothing");
+};
+Names* N = nullptr;
+
+// The scratch of the losses and that of all other calls are laid out differently, and each has words that must be zero between calls.
+bool of_losses(PyObject* workspace) { return PyObject_TypeCheck(workspace, (PyTypeObject*)g_loss_workspace); }
+struct Scratch {
+  void* ptr;
+  size_t bytes;
+  explicit Scratch(PyObject* workspace) {
+    if (of_losses(workspace)) fail(PyExc_TypeError, "workspace must be a Workspace (a LossWorkspace is laid out differently)");
+    ptr = (void*)int_attr(workspace, N->ptr);
+    bytes = int_attr(workspace, N->bytes);
+  }
+};
+void* stream() { return (void*)c10::hip::getCurrentHIPStream().stream(); }
 
 // An output: the caller's tensor, checked, or a new one.
 struct Output {
@@ -175,20 +202,6 @@ struct Output {
   }
 };
 
-struct Names {
-  PyObject *ptr = intern("ptr"), *bytes = intern("bytes"), *B = intern("B"), *cap = intern("cap"), *T_G = intern("T_G"),
-           *ent_sum = intern("ent_sum"), *ent_cnt = intern("ent_cnt"), *LA = intern("LA"), *LR = intern("LR"),
-           *nA = intern("nA"), *nR = intern("nR"), *mom = intern("mom"), *n_accept = intern("n_accept"),
-           *next_token = intern("next_token"), *H_p = intern("H_p"), *H_q = intern("H_q"), *d_js = intern("d_js"),
-           *p_accept = intern("p_accept"), *accept_mask = intern("accept_mask"), *status = intern("status"),
-           *base_test = intern("base_test"), *reject_rule = intern("reject_rule"), *kde_min_n = intern("kde_min_n"),
-           *bw_rule = intern("bw_rule"), *relaxed_off = intern("relaxed_off"), *d_eps = intern("d_eps"),
-           *stats_path = intern("stats_path"), *apply_update = intern("apply_update"), *list_update = intern("list_update"),
-           *wait_polls = intern("wait_polls"), *buf = intern("buf"), *clip_low = intern("clip_low"), *clip_high = intern("clip_high"),
-           *kl_coef = intern("kl_coef"), *entropy_coef = intern("entropy_coef"), *kind = intern("kind"), *beta = intern("beta"),
-           *margin = intern("margin"), *label_smoothing = intern("label_smoothing");
-};
-Names* N = nullptr;
 
 const at::Tensor& draft_rows(PyObject* o) {
   const at::Tensor& x = tensor(o, "draft_logits");
@@ -222,8 +235,9 @@ PyObject* py_draft_entropy(PyObject*, PyObject* const* args, Py_ssize_t nargs, P
     const adasd_dtype dt = logits_type(a[0]);
     const int step = (int)integer(a[4], 0), k_max = (int)integer(a[5], 1 << 30);
     const int64_t stride = B > 1 ? x.stride(0) : V;
-    void *ws = (void*)int_attr(a[1], N->ptr), *st = stream(), *rows = x.data_ptr();
-    const size_t ws_bytes = int_attr(a[1], N->bytes);
+    const Scratch scratch(a[1]);
+    void *ws = scratch.ptr, *st = stream(), *rows = x.data_ptr();
+    const size_t ws_bytes = scratch.bytes;
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = g_abi.draft_entropy(rows, dt, B, V, stride, tg, active, step, k_max, (float*)H.ptr, (uint8_t*)stop.ptr, ws, ws_bytes, st);
@@ -258,8 +272,9 @@ PyObject* py_draft_step(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyOb
     const uint64_t seed = integer(a[6], 0);
     const uint32_t round0 = (uint32_t)integer(a[9], 0);
     const int64_t stride = B > 1 ? x.stride(0) : V;
-    void *ws = (void*)int_attr(a[1], N->ptr), *st = stream(), *rows = x.data_ptr();
-    const size_t ws_bytes = int_attr(a[1], N->bytes);
+    const Scratch scratch(a[1]);
+    void *ws = scratch.ptr, *st = stream(), *rows = x.data_ptr();
+    const size_t ws_bytes = scratch.bytes;
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = g_abi.draft_step(rows, dt, B, V, stride, tg, active, step, k_max, seed, seq, rounds, round0, (float*)H.ptr,
@@ -364,8 +379,9 @@ PyObject* py_verify(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject
     v.status = (uint32_t*)raw(out, N->status);
     const bool noalloc = a[3] == Py_None;
     if (!noalloc) {
-      v.workspace = (void*)int_attr(a[3], N->ptr);
-      v.ws_bytes = int_attr(a[3], N->bytes);
+      const Scratch scratch(a[3]);
+      v.workspace = scratch.ptr;
+      v.ws_bytes = scratch.bytes;
     }
     void* st = stream();
     int rc;
@@ -416,6 +432,7 @@ struct RowsCall {
     rows.seq_stride = z->stride(0);
     rows.pos_stride = dims == 2 ? z->stride(1) : V;
     rows.tokens = (const int32_t*)input(tokens, at::kInt, "tokens");
+    if (!of_losses(workspace)) fail(PyExc_TypeError, "workspace must be a LossWorkspace");
     Ref buf(workspace, N->buf);
     if (tensor(buf.o, "workspace.buf").device() != z->device()) fail(PyExc_ValueError, "workspace must be on the logits' device");
     allocator = THPVariable_Unpack(buf.o).storage().allocator();
@@ -672,15 +689,17 @@ PyObject* py_preference_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs,
   });
 }
 
-// connect_losses(PolicyResult, PreferenceResult, addresses of token_logprob, token_logprob_grad, policy_loss, preference_loss)
+// connect_losses(PolicyResult, PreferenceResult, LossWorkspace, addresses of token_logprob, token_logprob_grad, policy_loss, preference_loss)
 PyObject* py_connect_losses(PyObject*, PyObject* args) {
-  PyObject *policy, *preference;
+  PyObject *policy, *preference, *workspace;
   unsigned long long f[4];
-  if (!PyArg_ParseTuple(args, "OOKKKK", &policy, &preference, &f[0], &f[1], &f[2], &f[3])) return nullptr;
+  if (!PyArg_ParseTuple(args, "OOO!KKKK", &policy, &preference, &PyType_Type, &workspace, &f[0], &f[1], &f[2], &f[3])) return nullptr;
   Py_INCREF(policy);
   Py_INCREF(preference);
   Py_XSETREF(g_policy_result, policy);
+  Py_INCREF(workspace);
   Py_XSETREF(g_preference_result, preference);
+  Py_XSETREF(g_loss_workspace, workspace);
   g_abi.token_logprob = (decltype(g_abi.token_logprob))f[0];
   g_abi.token_logprob_grad = (decltype(g_abi.token_logprob_grad))f[1];
   g_abi.policy_loss = (decltype(g_abi.policy_loss))f[2];

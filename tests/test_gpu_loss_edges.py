@@ -350,3 +350,23 @@ def test_tensors_written_to_are_known_to_torch(am):  # noqa: F811
         y = c.z.cuda()
         am.policy_loss(y, x, one, ws, dlogits=y)
     am.policy_loss(y, x, one, ws, dlogits=y)                 # (an inference tensor has no version)
+
+
+def test_workspaces_of_the_other_kind_are_refused(am):  # noqa: F811
+    """The scratch of verification and drafting, and that of the losses, are laid out differently."""
+    B, K, V = 2, 3, 512
+    c = Case(B, K, V, F, seed=63)
+    z, x, one = c.z.cuda(), c.x.cuda(), torch.ones(B, K, device="cuda")
+    ws, lws = am.Workspace(B, K, V, F), am.LossWorkspace(B, K, V, F)
+    target = torch.randn(B, K + 1, V, device="cuda")
+    for bad in (lambda: am.token_logprob(z, x, ws), lambda: am.token_logprob_grad(z, x, ws, one), lambda: am.policy_loss(z, x, one, ws),
+                lambda: am.preference_loss(z, x, ws), lambda: am.token_logprob(z, x, None), lambda: am.draft_entropy(z[:, 0], lws),
+                lambda: am.draft_step(z[:, 0], lws), lambda: am.verify(target, z, x, lws),
+                lambda: am.verify_shard_stats(target, z, x, lws, am.Shard(1, 0, V, 0))):
+        with pytest.raises(TypeError, match="orkspace"):
+            bad()
+
+    class Mine(am.LossWorkspace):
+        pass
+    assert am.token_logprob(z, x, Mine(B, K, V, F))[0].shape == (B, K)
+#--END
