@@ -67,8 +67,10 @@ enum {
 /* Per-sequence status bits written by adasd_verify / adasd_update_thresholds. */
 enum {
   ADASD_ST_BAD_TOKEN = 1u,   /* a draft token id was outside [0,V): that position fails the base test */
-  ADASD_ST_NONFINITE = 2u,   /* a needed row held NaN/+inf or no finite logit: its statistics are NaN,
-                                the position is rejected, a token drawn from such a row is -1 */
+  ADASD_ST_NONFINITE = 2u,   /* a needed row held NaN/+inf or no finite logit (where all are below -2^29 they
+                                need not count as such): its statistics are NaN, the position is rejected, a
+                                token drawn from such a row is -1.  Beside other logits, those masked with -inf or
+                                with any finite value far below them have no mass */
   ADASD_ST_ZERO_MASS = 4u,   /* max(0, p - q) had no mass at the rejected position: token drawn from p */
   ADASD_ST_OVERFLOW = 8u,    /* a history list was full: the append was dropped */
   ADASD_ST_EXACT_PATH = 16u, /* informational: the float64 tie-resolution path chose the token */

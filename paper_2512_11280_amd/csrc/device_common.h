@@ -11,7 +11,11 @@ constexpr int kBlock = 256;                 // threads per workgroup (4 wavefron
 constexpr int kWaves = kBlock / 64;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr double kLn2 = 0.693147180559945309417232;
-constexpr float kNegHuge = -3.0e38f;        // finite stand-in for "no element seen yet"
+// The lowest reference that a part of a row has its sums about: that of a part without an element, and of one that holds nothing but logits below it
+// (masks), which have no mass then.  A reference that followed them would be off by up to a unit in its last place, from here on an exponent
+// past the type's range: an infinite sum, times the 0 that brings it to the other parts' reference.  (-2^31 - 2^8: odd, as the references of hand-off
+// words are.)
+constexpr float kNegHuge = -2147483904.f;
 
 // Kernel arguments are fetched with scalar loads where they are first needed, one 64-byte line at a
 // time, and right after a launch every line misses all the way to memory: a kernel with a few
@@ -48,6 +52,11 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }  // v_exp_f32
 __device__ __forceinline__ float lg2(float x) { return __builtin_amdgcn_logf(x); }   // v_log_f32
+
+// A part's sums about a reference d higher: s part_factor(d), part_weighted(u, s, d) part_factor(d).  (Where the factor is 0 the product d s must not
+// leave the type's range; and a d of more than 64 comes of the bit that a reference gives to the flag of the hand-off words, of one below -2^30.)
+__device__ __forceinline__ float part_factor(float d) { return d > 64.f ? 0.f : ex2(d); }
+__device__ __forceinline__ float part_weighted(float u, float s, float d) { return u + fmaxf(d, -200.f) * s; }
 
 // log2 of a positive finite float, as exponent + hardware log2 of the mantissa in [0.5, 1): absolute
 // error about 6e-8 whatever the magnitude.  A handful of instructions, where the double-precision
@@ -261,11 +270,11 @@ __device__ __forceinline__ Lse lse_empty() { return Lse{kNegHuge, 0.f, 0.f}; }
 __device__ __forceinline__ Lse lse_merge(const Lse& a, const Lse& b) {
   float m = fmaxf(a.m, b.m);
   float da = a.m - m, db = b.m - m;          // <= 0, finite unless a row holds +inf (then NaN: flagged later)
-  float fa = ex2(da), fb = ex2(db);
+  float fa = part_factor(da), fb = part_factor(db);
   Lse r;
   r.m = m;
   r.s = a.s * fa + b.s * fb;
-  r.u = (a.u + da * a.s) * fa + (b.u + db * b.s) * fb;
+  r.u = part_weighted(a.u, a.s, da) * fa + part_weighted(b.u, b.s, db) * fb;
   return r;
 }
 
@@ -406,7 +415,7 @@ template <int DT> __device__ __forceinline__ uint4 neutral_vec() {   // all logi
                           : make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u);
 }
 
-// Largest finite logit held in NV vectors, times log2(e) (kNegHuge if there is none).
+// Largest finite logit held in NV vectors, times log2(e), or (there is none, or it is as low) something no higher than kNegHuge.
 // bf16 pairs are compared as packed f16: both formats order their bit patterns the same way, and
 // the bf16 patterns of +-inf / NaN and of anything from 2^121 on in size read as f16 NaNs, which the packed max ignores (those below 2^125 are
 // signalling ones: see maxima_without_nans).
@@ -435,7 +444,7 @@ template <int DT, int NV> __device__ __forceinline__ float vecs_max(const uint4 
       float c = __uint_as_float(v[j].z), d = __uint_as_float(v[j].w);
       m = fmaxf(m, fmaxf(fmaxf(a, b), fmaxf(c, d)));   // NaN-ignoring; +inf surfaces in the sums
     }
-    return (m > kNegHuge && m < INFINITY) ? m * kLog2e : kNegHuge;
+    return m < INFINITY ? m * kLog2e : kNegHuge;
   }
 }
 

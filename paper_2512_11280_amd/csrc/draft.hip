@@ -20,8 +20,8 @@ template <bool DRAW> __device__ __forceinline__ void fold_wave(Lse& l, Top2& t) 
   if (DRAW) wave_max2(top, best);              // (one chain of exchanges for both)
   else top = wave_max_f(top);
   const float M = __uint_as_float(__float_as_uint(top) | 1u);
-  const float d = top > kNegHuge ? l.m - M : 0.f, f = ex2(d);     // (nothing finite seen: the sums are 0, or a NaN)
-  float a = l.s * f, b = (l.u + d * l.s) * f;
+  const float d = l.m - M, f = part_factor(d);
+  float a = l.s * f, b = part_weighted(l.u, l.s, d) * f;
   swap32(a, b);
   float x = a + b, y = x;
   swap16(x, y);
@@ -38,9 +38,9 @@ template <bool DRAW> __device__ __forceinline__ void fold_workgroup(const Lse (&
   float s[kWaves], u[kWaves];
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    const float d = M > kNegHuge ? ls[w].m - M : 0.f, f = ex2(d);
+    const float d = ls[w].m - M, f = part_factor(d);
     s[w] = ls[w].s * f;
-    u[w] = (ls[w].u + d * ls[w].s) * f;
+    u[w] = part_weighted(ls[w].u, ls[w].s, d) * f;
   }
   l = Lse{__uint_as_float(__float_as_uint(M) | 1u), (s[0] + s[1]) + (s[2] + s[3]), (u[0] + u[1]) + (u[2] + u[3])};
   if (DRAW) t = top2_merge(top2_merge(ts[0], ts[1]), top2_merge(ts[2], ts[3]));
@@ -57,7 +57,7 @@ template <int DT> __device__ __forceinline__ Lse wave_row_sums(const char* row, 
     if (z < INFINITY) top = fmaxf(top, z);
   }
   top = wave_max_f(top);
-  const float m = top > kNegHuge ? top * kLog2e : kNegHuge;
+  const float m = fmaxf(top * kLog2e, kNegHuge);
   double s = 0.0, u = 0.0;
 #pragma unroll 1
   for (int v = lane; v < V; v += 64) {

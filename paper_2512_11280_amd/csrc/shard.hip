@@ -27,8 +27,8 @@ __global__ void __launch_bounds__(kBlock) k_shard_fold_rows(RowMap map, int S, W
     const float4 p = ws.part1[(size_t)rho * kMaxSplit + lane];
     t = Lse{p.x, p.y, p.z};
   }
-  const float M = wave_max_f(t.m), d = t.m - M, f = ex2(d);
-  const float sw = wave_sum_f(t.s * f), uw = wave_sum_f((t.u + d * t.s) * f);
+  const float M = wave_max_f(t.m), d = t.m - M, f = part_factor(d);
+  const float sw = wave_sum_f(t.s * f), uw = wave_sum_f(part_weighted(t.u, t.s, d) * f);
   if (lane == 0) out[rho] = make_float4(M, sw, uw, 0.f);
 }
 

@@ -95,8 +95,8 @@ k_rowstats(RowMap map, int S, Workspace ws) {
   // wavefront fold: common reference, then plain sums
   Lse st = lse_merge(Lse{M, s0 + s1, u0 + u1}, extra);
   {
-    const float Mw = wave_max_f(st.m), d = st.m - Mw, f = ex2(d);
-    const float sw = wave_sum_f(st.s * f), uw = wave_sum_f((st.u + d * st.s) * f);
+    const float Mw = wave_max_f(st.m), d = st.m - Mw, f = part_factor(d);
+    const float sw = wave_sum_f(st.s * f), uw = wave_sum_f(part_weighted(st.u, st.s, d) * f);
     st = Lse{Mw, sw, uw};
   }
 

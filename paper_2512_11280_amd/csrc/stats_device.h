@@ -81,8 +81,8 @@ __device__ __forceinline__ RowResult finish_row(const Lse& t) {
 // Fold of up to 64 partial states of one row held one per lane (an empty state in the other lanes), by
 // one wavefront; all lanes return the same.
 __device__ __forceinline__ RowResult fold_lanes(const Lse& t) {
-  const float M = wave_max_f(t.m), d = t.m - M, f = ex2(d);
-  return finish_row(Lse{M, wave_sum_f(t.s * f), wave_sum_f((t.u + d * t.s) * f)});
+  const float M = wave_max_f(t.m), d = t.m - M, f = part_factor(d);
+  return finish_row(Lse{M, wave_sum_f(t.s * f), wave_sum_f(part_weighted(t.u, t.s, d) * f)});
 }
 
 // Fold of the S slice results that the first statistics kernel left for one row.

@@ -137,8 +137,8 @@ __device__ __forceinline__ void record_rows(const SliceRecord& o, Lse& tp, Lse& 
 __device__ __forceinline__ Lse fold_pair(const Lse& tp, const Lse& tq) {
   float mp = tp.m, mq = tq.m;
   wave_max2(mp, mq);
-  const float dp = tp.m - mp, dq = tq.m - mq, ep = ex2(dp), eq = ex2(dq);
-  float s = wave_sum4(tp.s * ep, tq.s * eq, (tp.u + dp * tp.s) * ep, (tq.u + dq * tq.s) * eq), u = s;
+  const float dp = tp.m - mp, dq = tq.m - mq, ep = part_factor(dp), eq = part_factor(dq);
+  float s = wave_sum4(tp.s * ep, tq.s * eq, part_weighted(tp.u, tp.s, dp) * ep, part_weighted(tq.u, tq.s, dq) * eq), u = s;
   swap16(s, u);
   return Lse{(threadIdx.x & 32) ? mq : mp, s, u};
 }
@@ -178,6 +178,13 @@ __device__ __forceinline__ float phase1_sums(const uint4 (&xp)[NB], const uint4 
   return wave_sum4(s[0][0] + s[0][1], s[1][0] + s[1][1], u[0][0] + u[0][1], u[1][0] + u[1][1]);
 }
 
+// The reference of a wavefront's sums: its largest logit's, with the bit set that says that a record is there.  Below -2^30 that bit is an exponent of
+// 128: nothing has mass there then (what the other wavefronts of a row with masks have is above it).
+__device__ __forceinline__ float reference_of(float m) {
+  m = fmaxf(m, kNegHuge);
+  const float r = flagged(m);
+  return r != m && m < -0x1p30f ? -(0x1p30f + 0x1p7f) : r;
+}
 // Phase 1 of the slice held in (xp, xq) by the whole workgroup.  In wavefront 0 the lower half of the lanes
 // returns the target row's (m, s, u), the upper half the draft row's; the other wavefronts return nothing of
 // use.  One workgroup barrier.  masked: whether a logit of -inf (or a NaN) was met by this wavefront.
@@ -188,8 +195,8 @@ __device__ __forceinline__ Lse phase1(int s, const FusedGeom& g, uint4 (&xp)[NB]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float mp = vecs_max<DT, NB>(xp), mq = vecs_max<DT, NB>(xq);
   wave_max2(mp, mq);
-  mp = flagged(mp);
-  mq = flagged(mq);
+  mp = reference_of(mp);
+  mq = reference_of(mq);
   pad_slice<DT, T, NB>(s, g, xp, xq);
   const int left = wave_left(s, g);
   float sum = phase1_sums<DT, T, NB, false, SKIP>(xp, xq, -mp, -mq, left);
