@@ -99,6 +99,7 @@ struct DraftShared {
 // the slices' records, and with DRAW settles a winner that does not lead by more than the rounding guard.
 template <int DT, bool DRAW, bool PRUNE>
 __global__ void __launch_bounds__(kBlock, 7) k_draft(RowMap map, int S, int chunk, Workspace ws, DraftOut dout, DraftDraw dr) {
+  if (DT == ADASD_BF16) maxima_without_nans();
   warm_kernargs<sizeof(RowMap) + 2 * sizeof(int) + sizeof(Workspace) + sizeof(DraftOut) + sizeof(DraftDraw)>();
   constexpr int EPV = Elem<DT>::per_vec;
   __shared__ DraftShared sh;

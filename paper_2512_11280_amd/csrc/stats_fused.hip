@@ -307,6 +307,7 @@ __device__ __forceinline__ void fold_position(const Lse& tp, const Lse& tq, JsNo
 template <int DT, int T, int NB, bool SKIP>
 __global__ void __launch_bounds__(T, NB <= 4 ? 8 : 4)
 k_stats_fused(RowMap map, FusedGeom g, Workspace ws, VerifyOut vout, HistArgs hist) {
+  if (DT == ADASD_BF16) maxima_without_nans();
   warm_kernargs<sizeof(RowMap) + sizeof(FusedGeom) + sizeof(Workspace) + sizeof(VerifyOut) + sizeof(HistArgs)>();
   constexpr int W = T / 64;
   __shared__ FusedShared<W> sh;

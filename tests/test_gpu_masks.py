@@ -8,7 +8,7 @@ import torch
 pytestmark = pytest.mark.gpu
 
 BF, F = torch.bfloat16, torch.float32
-MASKS = {BF: [-1e4, -5e8, -8e8, -1e9, -1.2e9, -1e10, -3e12, -1e30, -2.5e36, -1e38, -2e38, torch.finfo(BF).min],
+MASKS = {BF: [-1e4, -5e8, -8e8, -1e9, -1.2e9, -1e10, -3e12, -1e30, -2.5e36, -5e36, -9e36, -2e37, -1e38, -2e38, torch.finfo(BF).min],
          F: [-1e4, -5e8, -8e8, -1e9, -1.2e9, -1e10, -3e12, -1e30, -1e37, -1e38, -2e38, torch.finfo(F).min]}
 
 
