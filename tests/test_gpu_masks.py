@@ -69,3 +69,22 @@ def test_rows_that_are_masked_throughout(am, value, dtype, stats_path):
         r = am.verify(z, d, x, ws, seed=7, options=am.Options(stats_path=stats_path))
         assert (r.H_p - math.log(V)).abs().max() < 1e-5 * math.log(V) and not (r.status & 2).any()
         assert (r.d_js >= 0).all() and r.d_js.max() <= 1e-5 * math.log(V) / math.log(2)
+
+
+@pytest.mark.parametrize("dtype, mask", [(d, m) for d in (BF, F) for m in MASKS[d]])
+def test_column_shards_that_are_masked(am, mask, dtype):
+    """The same where whole column slices hold nothing but masked logits: the statistics of every position (what is accepted may differ: a drafted
+    token masked in both rows has the ratio 0 / 0 with -inf and that of two numbers otherwise), and no row is broken."""
+    from paper_2512_11280_amd import workloads as wl
+    from test_gpu_parity import _sharded_decisions, _sharded_tokens
+    got = []
+    for value in (-math.inf, mask):
+        batch = wl.config_batched(B=3, k=4, V=9000, dtype=dtype, seed=11, cap=96)
+        batch.target[..., 2000:7000] = value
+        batch.draft[..., 2000:7000] = value
+        ctx = _sharded_decisions(am, batch, 5, options=am.Options(apply_update=1))
+        _sharded_tokens(am, batch, ctx, ctx[0])
+        got.append(ctx[0])
+    for a, b in zip(*got):
+        assert all(torch.equal(getattr(a, n), getattr(b, n)) for n in ("H_p", "H_q", "d_js"))
+        assert not (b.status & 2).any() and (b.next_token >= 0).all()
