@@ -892,14 +892,18 @@ hipError_t launch_loss(const LossRows& rows, int dt, LossTerm f, const LossWorks
     if (dt == DTV && ref == REFV && plan.nb == NBV && plan.wpr == WPRV && past == PASTV) \
       launch_kernel((k_loss_join<DTV, REFV, NBV, WPRV, PASTV>), dim3(groups), dim3(WPRV > kWaves ? 64 * WPRV : kBlock), st, \
                     JoinArgs{some, f, ws, plan.S, plan.chunk, ent ? 1 : 0, early ? 1 : 0});
+#define ADASD_JOIN_FEW(REFV, NBV, WPRV) \
+    ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, false) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, false)
 #define ADASD_JOIN_CASES(REFV, NBV, WPRV) \
-    ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, false) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, false) \
-    ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, true) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, true)
+    ADASD_JOIN_FEW(REFV, NBV, WPRV) ADASD_JOIN_CASE(ADASD_BF16, REFV, NBV, WPRV, true) ADASD_JOIN_CASE(ADASD_F32, REFV, NBV, WPRV, true)
     ADASD_JOIN_CASES(false, 4, 1) ADASD_JOIN_CASES(false, 8, 1) ADASD_JOIN_CASES(false, 16, 1) ADASD_JOIN_CASES(false, 16, 2)
-    ADASD_JOIN_CASES(false, 16, 4) ADASD_JOIN_CASES(false, 8, 4) ADASD_JOIN_CASES(false, 8, 8)
+    ADASD_JOIN_CASES(false, 8, 4) ADASD_JOIN_CASES(false, 8, 8)
     ADASD_JOIN_CASES(true, 2, 1) ADASD_JOIN_CASES(true, 4, 1) ADASD_JOIN_CASES(true, 8, 1) ADASD_JOIN_CASES(true, 8, 2)
-    ADASD_JOIN_CASES(true, 8, 4) ADASD_JOIN_CASES(true, 8, 8) ADASD_JOIN_CASES(true, 4, 4)
+    ADASD_JOIN_CASES(true, 8, 4) ADASD_JOIN_CASES(true, 8, 8)
+    // (of few rows alone: 1024 slices of 4096 vectors, 64 MiB, at the most; 1280 of 1024)
+    ADASD_JOIN_FEW(false, 16, 4) ADASD_JOIN_FEW(true, 4, 4)
 #undef ADASD_JOIN_CASES
+#undef ADASD_JOIN_FEW
 #undef ADASD_JOIN_CASE
   } else if (n > 0) {
     const int S = scan_split(n, rows.V, dt), chunk = slice_chunk(nv, S);
