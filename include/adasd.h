@@ -384,7 +384,8 @@ int adasd_update_thresholds(const adasd_state *st /* host */, int k_max, const i
  *                    finite logit, or a largest one beyond 2^26 in size: results NaN; a reference's row likewise), or 0.  A
  *                    gradient row that depends on a NaN is NaN, one that depends on the log-probability of a token outside
  *                    the vocabulary too.
- * Logits of -inf, or of the type's lowest value beside ordinary ones, are tokens without mass: gradient 0 there.
+ * Logits of -inf, or of any finite value far below the row's largest (a mask of -1e4, -1e9, the type's lowest, ...), are tokens
+ * without mass: gradient 0 there.
  * Gradients have the type of the logits (formed in 32 bits, rounded once).  dlogits may be the logits' own memory (same pointer and
  * strides: the gradient takes their place); any other address range that overlaps that of logits the call reads is refused.
  * Strides as everywhere here are in elements; rows may lie in either order (a [T,B,V] array seen as [B,T,V] is fine, and so is a
@@ -429,8 +430,9 @@ int adasd_token_logprob_grad(const adasd_rows *rows /* host */, const float *dlo
  * Clipped policy loss.  With r = exp(logprob - old_logprob) and the advantage A of the position,
  *   term = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A) + kl_coef KL - entropy_coef H,   loss = sum over (b,t) of weight term,
  *   KL   = exp(d) - 1 - d with d = ref_logprob - logprob (the sampled token's estimate; +inf at d = +-inf), or, with ref_logits,
- *          sum_j p_j (ln p_j - ln q_j) over the vocabulary (+inf where q_j = 0 < p_j; such a row's gradient is NaN; a p_j below
- *          2^-149 of the row's largest is 0), or 0 without either.  (Both given: ADASD_ERR_INVALID_ARG.)
+ *          sum_j p_j (ln p_j - ln q_j) over the vocabulary (+inf where q_j = 0 < p_j, or where a difference of two logits
+ *          leaves the range of float; such a row's gradient is NaN; a p_j below 2^-126 of the row's largest may count as 0), or 0
+ *          without either.  (Both given: ADASD_ERR_INVALID_ARG.)
  * Where A is 0 the first part is 0 whatever r is; a coefficient of 0 leaves its part out.  dlogits is the derivative of
  * grad_scale * loss; at a border of the clipping the unclipped branch counts.
  */
