@@ -215,7 +215,7 @@ struct LossTerm {       // what the numbers of a position are formed from
   WordWait wait;                // for the slices' records (see hand_off)
 };
 struct LossCoef {       // of a position: its gradient row is a 1[j = x] + 2^(x_j - m) (k0 + k1 (x_j - m) + k2 dd_j) (loss_device.h)
-  float m, a, k0, k1, k2, c, pad[2];
+  float m, a, k0, k1, k2, mr, pad[2];
 };
 struct LossWorkspace {
   uint64_t* sets;       // [positions] arrival words of the rows cut into slices (records.h), zero between launches

@@ -61,7 +61,6 @@ __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const 
   const bool odd = threadIdx.x & 1;
   const bool known = in.x >= 0 && in.x < rows.V;
   const LossRow row = finish_loss_row<REF>(sums);
-  const float c = REF ? c_of(sums.m, sums.mr) : 0.f;
   const double lp = known ? (double)in.z - row.lse : (double)NAN;
   const double w = (double)in.weight;
   double a = 0.0, by_entropy = 0.0, by_kl = 0.0, loss = 0.0, kl = row.kl;
@@ -111,10 +110,10 @@ __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const 
     k.k1 = (float)(-by_entropy * kNat * row.inv_s);
   }
   if (REF && by_kl != 0.0) {
-    k0 += by_kl * (kNat * (double)c - (row.lse - row.lse_ref) - row.kl);
+    k0 -= by_kl * (row.apart + row.kl);
     k.k2 = (float)(by_kl * kNat * row.inv_s);
   }
-  k.c = c;
+  k.mr = REF ? sums.mr : 0.f;
   k.a = (float)a;
   k.k0 = k0 == 0.0 ? 0.f : (float)(k0 * row.inv_s);      // (nothing of the row enters a gradient of zeros)
   k.m = fabsf(k.k0) < INFINITY ? sums.m : __uint_as_float(0x7fc00001u);      // (every element of a gradient that is no number is none)
@@ -485,7 +484,7 @@ template <int DT> __device__ __forceinline__ void store_grad(char* row, int idx,
 // The gradients of one vector, but for the token's a: e (k0 + k1 t + k2 dd).  (Where e is 0 they are 0; a row whose k0 is no number has no m either.)
 template <int DT, bool ENT, bool REF>
 __device__ __forceinline__ void grad_vec(const uint4& x, const uint4& xr, const LossCoef& k, float (&g)[Elem<DT>::per_vec]) {
-  const float neg_m = -k.m;
+  const float neg_m = -k.m, neg_mr = -k.mr;
 #pragma unroll
   for (int h = 0; h < Elem<DT>::per_vec / 4; ++h) {
     float z[4], t[4], e[4], q[4];
@@ -499,7 +498,7 @@ __device__ __forceinline__ void grad_vec(const uint4& x, const uint4& xr, const 
       float y[4];
       unpack4<DT>(xr, h, y);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) q[i] = fmaf(k.k2, fma_log2e(z[i] - y[i], -k.c), q[i]);
+      for (int i = 0; i < 4; ++i) q[i] = fmaf(k.k2, t[i] - fma_log2e(y[i], neg_mr), q[i]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) g[4 * h + i] = ENT || REF ? mass_times(e[i], q[i]) : e[i] * q[i];
@@ -611,7 +610,7 @@ __device__ __forceinline__ bool await_result(uint64_t* at, WordWait wait, LossCo
   if (lane < kResultWords) __hip_atomic_store(at + lane, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   k.m = lane_value(word_lo(w), 0);
   k.a = lane_value(word_hi(w), 0);
-  k.c = lane_value(word_lo(w), 1);
+  k.mr = lane_value(word_lo(w), 1);
   k.k0 = lane_value(word_hi(w), 1);
   k.k1 = lane_value(word_hi(w), 2);
   k.k2 = lane_value(word_hi(w), 3);
@@ -622,7 +621,7 @@ __device__ __forceinline__ uint64_t send_results(uint64_t* at, int S, int own, c
   const int lane = threadIdx.x & 63;
   if (lane >= S || lane == own) return 0;
   at += lane * kResultWords;
-  __hip_atomic_store(at + 1, record_word(bits_of(k.c) | 1u, k.k0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(at + 1, record_word(bits_of(k.mr) | 1u, k.k0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __hip_atomic_store(at + 2, record_word(1u, k.k1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __hip_atomic_store(at + 3, record_word(1u, k.k2), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return __hip_atomic_exchange(at, record_word(bits_of(k.m), k.a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

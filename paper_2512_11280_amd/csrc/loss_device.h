@@ -2,12 +2,12 @@
 //
 // With x = z log2(e) (the float constant, see finish_loss_row) and m the largest x of the row, e_j = 2^(x_j - m):
 //   s = sum e_j,   u = sum (x_j - m) e_j            log-normaliser and entropy,
-//   w = sum e_j dd_j,  dd_j = (z_j - zr_j) log2(e) - c   (reference row zr) for the KL over the vocabulary.
-// Any constant c gives the same KL, but for rounding: the terms have the size of c less what the rows' log ratio typically is.  c is the
-// difference of the two references (c_of), which is near it wherever the rows have mass.
+//   w = sum e_j dd_j,  dd_j = (x_j - m) - (xr_j - mr)   (reference row zr, with its own mr) for the KL over the vocabulary.
+// Each logit is taken about its own row's reference first: softmax does not see a row's offset, and the difference of two logits with different ones has
+// lost what the KL is formed from (offsets of 300 and -300: 1e-3 of the KL, of 3e5 a tenth).
 // The gradient of every loss here with respect to a row is
 //   dz_j = a 1[j = x] + e_j (k0 + k1 (x_j - m) + k2 dd_j)
-// with five numbers per position: a is the derivative by the token's log-probability, k0 gathers -a and the constants of the
+// with m, mr and four numbers per position: a is the derivative by the token's log-probability, k0 gathers -a and the constants of the
 // entropy's and the KL's derivatives, k1 is the entropy's, k2 the KL's coefficient, all three over s.
 #pragma once
 #include "internal.h"
@@ -16,7 +16,7 @@
 namespace adasd {
 
 struct LossSums {          // of a slice
-  float m, s, u, w;        // of the row (w about c_of)
+  float m, s, u, w;        // of the row
   float mr, sr;            // of the reference's row
 };
 // Every reference has its lowest bit set (the flag of the hand-off words), from the first on: brought about afterwards it would cost each fold
@@ -29,11 +29,6 @@ constexpr float kLargestM = 67108864.f * kLog2e + 16.f;
 // logits, they would be off by up to a unit in their last place, which from 2^31 on is an exponent past the type's range; and the difference of two
 // of them times a sum would pass it in the folds.  (-2^27: a unit is 16 there, e at most 2^24.)
 constexpr float kLowestM = -134217728.f;
-// What w is about, as the sums' references are: a part's own, brought to another's in the folds.  (Odd: it travels in a word that says itself that it is
-// there.)  It hangs on the rows' largest logits and on nothing else.  The difference of the token's two logits, which would be
-// nearer at times, is 1e9 where one of the two is masked, and all other terms are then differences of two such numbers.
-__device__ __forceinline__ float c_of(float m, float mr) { return odd_bit(m - mr); }
-static_assert(kLowestM < -kLargestM, "a row at the lowest reference is flagged");
 __device__ __forceinline__ LossSums loss_empty() { return LossSums{odd_bit(kLowestM), 0.f, 0.f, 0.f, odd_bit(kLowestM), 0.f}; }
 
 // e v, and 0 where e is 0, whatever v is (a token, or a part of a row, without mass: v may be infinite, or no number).  One instruction; a comparison, a selection
@@ -49,7 +44,7 @@ __device__ __forceinline__ float mass_times(float e, float v) {
 template <int DT, bool REF>
 __device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const uint4& xr) {
   constexpr int EPV = Elem<DT>::per_vec;
-  const float neg_m = -a.m, neg_mr = -a.mr, neg_c = REF ? -c_of(a.m, a.mr) : 0.f;
+  const float neg_m = -a.m, neg_mr = -a.mr;
   float s[2], u[2], w[2], sr[2];
   auto join = [](float& sum, float v, bool first) { sum = first ? v : sum + v; };
 #pragma unroll
@@ -74,7 +69,7 @@ __device__ __forceinline__ void loss_push_at(LossSums& a, const uint4& x, const 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         join(sr[i & 1], er[i], g == 0 && i < 2);
-        join(w[i & 1], mass_times(e[i], fma_log2e(z[i] - y[i], neg_c)), g == 0 && i < 2);
+        join(w[i & 1], mass_times(e[i], t[i] - tr[i]), g == 0 && i < 2);
       }
     }
   }
@@ -91,9 +86,9 @@ template <int DT, bool REF, int NV>
 __device__ __forceinline__ void loss_raise(LossSums& a, const uint4 (&x)[NV], const uint4 (&xr)[NV]) {
   const float m = odd_bit(fmaxf(a.m, vecs_max<DT, NV>(x))), d = a.m - m, f = ex2(d);
   if (REF) {
-    const float mr = odd_bit(fmaxf(a.mr, vecs_max<DT, NV>(xr)));
-    a.w = mass_times(f, fmaf(c_of(a.m, a.mr) - c_of(m, mr), a.s, a.w));
-    a.sr *= ex2(a.mr - mr);
+    const float mr = odd_bit(fmaxf(a.mr, vecs_max<DT, NV>(xr))), dr = a.mr - mr;
+    a.w = mass_times(f, fmaf(d - dr, a.s, a.w));
+    a.sr *= ex2(dr);
     a.mr = mr;
   }
   a.u = (a.u + d * a.s) * f;
@@ -112,9 +107,9 @@ template <bool REF> __device__ __forceinline__ LossSums loss_merge(const LossSum
   r.sr = 0.f;
   if (REF) {
     r.mr = fmaxf(a.mr, b.mr);
-    const float c = c_of(r.m, r.mr);
-    r.w = mass_times(fa, fmaf(c_of(a.m, a.mr) - c, a.s, a.w)) + mass_times(fb, fmaf(c_of(b.m, b.mr) - c, b.s, b.w));
-    r.sr = a.sr * ex2(a.mr - r.mr) + b.sr * ex2(b.mr - r.mr);
+    const float dra = a.mr - r.mr, drb = b.mr - r.mr;
+    r.w = mass_times(fa, fmaf(da - dra, a.s, a.w)) + mass_times(fb, fmaf(db - drb, b.s, b.w));
+    r.sr = a.sr * ex2(dra) + b.sr * ex2(drb);
   }
   return r;
 }
@@ -145,8 +140,9 @@ template <bool REF> __device__ __forceinline__ LossSums loss_fold_wave(const Los
   r.s = (float)wave_sum_d(a.s * f);
   if (REF) {
     r.mr = odd_bit(wave_max_f(a.mr));
-    r.w = (float)wave_sum_d(mass_times(f, fmaf(c_of(a.m, a.mr) - c_of(r.m, r.mr), a.s, a.w)));
-    r.sr = (float)wave_sum_d(a.sr * ex2(a.mr - r.mr));
+    const float dr = a.mr - r.mr;
+    r.w = (float)wave_sum_d(mass_times(f, fmaf(d - dr, a.s, a.w)));
+    r.sr = (float)wave_sum_d(a.sr * ex2(dr));
   }
   return r;
 }
@@ -155,7 +151,8 @@ template <bool REF> __device__ __forceinline__ LossSums loss_fold_wave(const Los
 // 1 / (1 + eps), eps = k ln 2 - 1 = -1.3e-8.  Dividing by k (and not by log2(e)) leaves an error of eps H in the
 // log-normaliser, which is put right; in the entropy it is of the size of eps.
 struct LossRow {
-  double lse, lse_ref;     // log-normalisers
+  double lse;              // log-normaliser
+  double apart;            // ln s - ln sr
   double H, kl;
   double inv_s;            // 1 / s
   bool bad;
@@ -172,14 +169,12 @@ template <bool REF> __device__ __forceinline__ LossRow finish_loss_row(const Los
   r.lse = kNat * ((double)t.m + l2) + kTemperature * r.H;
   r.inv_s = inv;
   r.bad = !ok;
-  r.lse_ref = 0.0;
-  r.kl = 0.0;
+  r.apart = r.kl = 0.0;
   if (REF) {
     const bool okr = t.sr > 0.f && t.sr < INFINITY && fabsf(t.mr) <= kLargestM;
     const double l2r = log2_fine(okr ? t.sr : NAN);
-    r.lse_ref = kNat * ((double)t.mr + l2r);
-    // (c next to the normalisers' difference: both large where the rows carry different offsets)
-    r.kl = fmax(kNat * ((double)t.w * inv + ((double)c_of(t.m, t.mr) - (((double)t.m - (double)t.mr) + (l2 - l2r)))), 0.0);
+    r.apart = kNat * (l2 - l2r);
+    r.kl = fmax(kNat * ((double)t.w * inv) - r.apart, 0.0);
     if (!ok || !okr || t.w != t.w) r.kl = (double)NAN;
     r.bad = r.bad || !okr;
   }

@@ -138,10 +138,9 @@ def test_masks_of_any_size(am, mask, dtype):  # noqa: F811
 
 
 def _kl_spread(z, zr, o):
-    """What the terms of the KL cancel from, no token's difference by itself: the sums are about differences of the two rows' largest logits
-    (of a lane, a slice, the row).  Such a difference is z_a - y_b, y_b >= y_a, for the lane's own largest z_a: off the typical difference by |D_a| and
-    what y_b is above y_a, which is at most |D_a| + |ln p_a| + |ln max q|.  Weighted by p: 2 KL-like sums, H, and the logarithms of
-    the two rows' sums about their largest."""
+    """What the terms of the KL cancel from, no token's difference by itself.  A term is t - tr, each logit about the largest of its own row (or part of
+    it): |t| = |ln p + ln s|, |tr| = |ln q + ln sr| <= |D| + |ln p| + |ln sr|.  Weighted by p and rounded a few times each (tol_kl and grad allow
+    more than 30 steps of it): KL-like sums, H, and the logarithms of the two rows' sums about their largest."""
     s, sr = (torch.logsumexp(v.double(), -1) - v.double().amax(-1) for v in (z, zr))
     return 2 * (o["p"] * o["D"].abs()).sum(-1) + o["H"] + s.abs() + sr.abs() + 1.0
 
@@ -369,4 +368,26 @@ def test_workspaces_of_the_other_kind_are_refused(am):  # noqa: F811
     class Mine(am.LossWorkspace):
         pass
     assert am.token_logprob(z, x, Mine(B, K, V, F))[0].shape == (B, K)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("offset", [0.0, 300.0, 3e4, 3e6, 3e7])
+def test_kl_of_rows_with_different_offsets(am, offset, dtype):  # noqa: F811
+    """Softmax does not see a row's offset: KL and gradient have the accuracy of rows without one.  (The type's rounding of the shifted logits
+    is part of the inputs.)"""
+    for B, T, V in ((2, 3, 40), (3, 5, 9001), (31, 43, 1037), (2, 3, 32003), (1, 1100, 5003)):
+        c = Case(B, T, V, dtype, seed=65, masked=0.0)
+        if dtype == BF:                                                             # (differences that the type still has at that size)
+            step = max(offset / 256, 1.0)
+            z, zref = (c.z.float() * step / 3 + offset).to(dtype), (c.z.float() * step / 3 + step * c.n(B, T, V).round() - offset).to(dtype)
+        else:
+            z, zref = c.z + offset, c.z + 0.5 * c.n(B, T, V) - offset
+        o = R.rows(z, c.x, zref)
+        o["spread"] = _kl_spread(z, zref, o)
+        r = am.policy_loss(z.cuda(), c.x.cuda(), torch.zeros(B, T, device="cuda"), c.ws(am), ref_logits=zref.cuda(),
+                           options=am.PolicyOptions(kl_coef=1.0))
+        assert not r.status.any()
+        R.near(r.kl, o["kl"], R.tol_kl(o), "kl")
+        g, tol = R.grad(o, torch.zeros(B, T), k=torch.ones(B, T), dtype=dtype)
+        R.near(r.dlogits, g, tol, "dlogits")
 #--END
