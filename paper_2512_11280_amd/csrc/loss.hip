@@ -8,7 +8,7 @@
 //   k_loss_sums  (slices of rows) the sums alone: log-probabilities, the preference loss, rows too long for k_loss_join.  One workgroup of
 //                a row folds its slices (hand_off).
 //   k_loss_grad  (pieces of rows) reads the logits again and forms the gradient.
-// Either way one wavefront settles the position: what is reported of it, and the five numbers of its gradient row.  Of few positions
+// Either way one wavefront settles the position: what is reported of it, and the six numbers of its gradient row.  Of few positions
 // the one done last adds up the loss, or settles its pair; of many k_loss_pairs and k_loss_total do.
 // Sums over positions and sequences are in 64 bits and in a fixed order, whoever forms them.
 #include "loss_device.h"

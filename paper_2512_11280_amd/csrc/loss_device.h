@@ -7,7 +7,7 @@
 // lost what the KL is formed from (offsets of 300 and -300: 1e-3 of the KL, of 3e5 a tenth).
 // The gradient of every loss here with respect to a row is
 //   dz_j = a 1[j = x] + e_j (k0 + k1 (x_j - m) + k2 dd_j)
-// with m, mr and four numbers per position: a is the derivative by the token's log-probability, k0 gathers -a and the constants of the
+// with six numbers per position (m and mr among them): a is the derivative by the token's log-probability, k0 gathers -a and the constants of the
 // entropy's and the KL's derivatives, k1 is the entropy's, k2 the KL's coefficient, all three over s.
 #pragma once
 #include "internal.h"
