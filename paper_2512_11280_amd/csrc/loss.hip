@@ -54,13 +54,13 @@ template <int DT> __device__ __forceinline__ void ask_logit(PositionIn& in, cons
 }
 
 // What is reported of a position, and the numbers of its gradient row, from the sums of the whole row.  Two neighbouring lanes (or more
-// pairs of them) go through it together; the one that `writes` reports.
+// pairs of them) go through it together; the one that `writes` reports.  exps: see finish_loss_row.
 template <bool REF>
 __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const LossTerm& f, int r, const PositionIn& in, const LossSums& sums,
-                                                    bool writes, double& term) {
+                                                    int exps, bool writes, double& term) {
   const bool odd = threadIdx.x & 1;
   const bool known = in.x >= 0 && in.x < rows.V;
-  const LossRow row = finish_loss_row<REF>(sums);
+  const LossRow row = finish_loss_row<REF>(sums, exps);
   const double lp = known ? (double)in.z - row.lse : (double)NAN;
   const double w = (double)in.weight;
   double a = 0.0, by_entropy = 0.0, by_kl = 0.0, loss = 0.0, kl = row.kl;
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(kBlock) k_loss_sums(SumsArgs args) {
     if (__builtin_expect(!arrived, 0)) a = wave_sums<DT, REF>(row, ref, V, 0, vectors_of<DT>(V));
   }
   double term;
-  const LossCoef k = settle_position<REF>(late.rows, f, r, in, a, lane == 0, term);
+  const LossCoef k = settle_position<REF>(late.rows, f, r, in, a, S > 1 ? 4 : 3, lane == 0, term);
   if (lane == 0) ws.coef[r] = k;
   position_done(late.rows, f, ws, r, term);
 }
@@ -745,7 +745,7 @@ k_loss_join(JoinArgs args) {
       if (settles) {
         role = kSettles;
         const bool writes = on_i && (RPB > 1 ? !(lane & 1) && lane < 2 * RPB : lane == 0);
-        const LossCoef settled = settle_position<REF>(rows, f, ri, in, a, writes, term);
+        const LossCoef settled = settle_position<REF>(rows, f, ri, in, a, WPR > 1 ? (S > 1 ? 4 : 3) : 2, writes, term);
         if (on_i) k = settled;
         else term = 0.0;
         if (RPB == 1 && S > 1) found = send_results(results, S, s, k);

@@ -131,7 +131,7 @@ __device__ __forceinline__ double wave_sum_d(float v) {
 }
 // One wavefront folds its lanes' sums; uniform results.  s (and sr and w, whose small difference the KL is) are folded in 64
 // bits, six roundings fewer each: the absolute error of a log-probability before its rounding 5.0e-8 rms for 6.5e-8 in the build that this came with, for
-// 0.3 us of 14 in a call of 193 rows; 3.6e-8 to 5.7e-8 now.
+// 0.3 us of 14 in a call of 193 rows; 3.4e-8 to 5.7e-8 now.
 template <bool REF> __device__ __forceinline__ LossSums loss_fold_wave(const LossSums& a) {
   LossSums r = a;
   r.m = odd_bit(wave_max_f(a.m));                // (a NaN's lowest bit may be lost on the way)
@@ -159,11 +159,16 @@ struct LossRow {
 };
 constexpr double kNat = 1.0 / (double)kLog2e;
 constexpr double kTemperature = (double)kLog2e * kLn2 - 1.0;
-template <bool REF> __device__ __forceinline__ LossRow finish_loss_row(const LossSums& t) {
+// The chip's 2^x is short by 3.4e-9 of itself on average (v_exp_f32, 2^28 arguments in [-1, 0], [-2, -1], [-16, 0]; 2.6e-8 rms).  A sum has that once from
+// its elements and once more from each fold that brought it here, `exps` times in all, but for the largest element, whose power is 1: added to the
+// normaliser, or the log-probabilities of a long sequence add up 1.4e-8 each.
+constexpr double kShort = 3.4e-9 / kLn2;
+__device__ __forceinline__ double log2_sum(float s, int exps) { return log2_fine(s) + exps * kShort * fmax(1.0 - 1.0 / (double)s, 0.0); }
+template <bool REF> __device__ __forceinline__ LossRow finish_loss_row(const LossSums& t, int exps) {
   LossRow r;
   const bool ok = t.s > 0.f && t.s < INFINITY && fabsf(t.u) < INFINITY && fabsf(t.m) <= kLargestM;
   const float s = ok ? t.s : NAN;
-  const double l2 = log2_fine(s), inv = 1.0 / (double)s;
+  const double l2 = log2_sum(s, exps), inv = 1.0 / (double)s;
   r.H = fmax(kNat * (l2 - (double)t.u * inv), 0.0);
   r.H = ok ? r.H : (double)NAN;
   r.lse = kNat * ((double)t.m + l2) + kTemperature * r.H;
@@ -172,7 +177,7 @@ template <bool REF> __device__ __forceinline__ LossRow finish_loss_row(const Los
   r.apart = r.kl = 0.0;
   if (REF) {
     const bool okr = t.sr > 0.f && t.sr < INFINITY && fabsf(t.mr) <= kLargestM;
-    const double l2r = log2_fine(okr ? t.sr : NAN);
+    const double l2r = log2_sum(okr ? t.sr : NAN, exps);
     r.apart = kNat * (l2 - l2r);
     r.kl = fmax(kNat * ((double)t.w * inv) - r.apart, 0.0);
     if (!ok || !okr || t.w != t.w) r.kl = (double)NAN;
