@@ -61,7 +61,7 @@ __device__ __forceinline__ LossCoef settle_position(const LossRows& rows, const 
   const bool odd = threadIdx.x & 1;
   const bool known = in.x >= 0 && in.x < rows.V;
   const LossRow row = finish_loss_row<REF>(sums, exps);
-  const double lp = known ? (double)in.z - row.lse : (double)NAN;
+  const double above = known ? (double)in.z - row.lse : (double)NAN, lp = above > 0.0 ? 0.0 : above;      // (a token with all the mass, to rounding)
   const double w = (double)in.weight;
   double a = 0.0, by_entropy = 0.0, by_kl = 0.0, loss = 0.0, kl = row.kl;
   term = 0.0;

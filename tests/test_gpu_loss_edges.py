@@ -412,4 +412,19 @@ def test_log_probabilities_have_no_bias(am, n, V, dtype):  # noqa: F811
     e = torch.cat([sums(70 + k) for k in range(max(1, 2000 // n))])
     assert e.pow(2).mean().sqrt() < 7e-8
     assert e.mean().abs() < 4 * 7e-8 / math.sqrt(e.numel()) + 2e-9
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_tokens_with_all_the_mass(am, dtype):  # noqa: F811
+    """Log-probabilities are not above 0 (nor ratios and scores formed from them), and entropies not below, by no rounding."""
+    for B, T, V in ((4, 64, 40), (4, 64, 5003), (2, 8, 128256), (40, 50, 1037)):
+        c = Case(B, T, V, dtype, seed=66, masked=0.0)
+        z = c.z.clone()
+        z.scatter_(-1, c.x.long()[..., None], (60.0 + 30.0 * torch.rand(B, T, 1, generator=torch.Generator().manual_seed(67))).to(dtype))
+        lp, H, _ = am.token_logprob(z.cuda(), c.x.cuda(), c.ws(am))
+        assert (lp <= 0).all() and (lp > -1e-6).all() and (H >= 0).all() and (H < 1e-5).all()
+        o = am.policy_loss(z.cuda(), c.x.cuda(), torch.ones(B, T, device="cuda"), c.ws(am), old_logprob=torch.zeros(B, T, device="cuda"))
+        assert (o.token_loss >= -1).all()
+        p = am.preference_loss(z.cuda(), c.x.cuda(), c.ws(am))
+        assert (p.score <= 0).all()
 #--END
